@@ -405,6 +405,79 @@ int zccl_compress_host(zccl_ctx* ctx, const float* x_host, size_t n, int eb_mode
 int zccl_decompress_host(zccl_ctx* ctx, const void* in_host, size_t in_bytes,
                          float* y_host, size_t y_capacity_elems, void* stream);
 
+/*
+ * Microscaled 4-bit floating point (MXFP4 of the OCP Microscaling Formats specification, version 1.0): the codec's sibling
+ * of fixed rate, 17 bits per 4 values, for operands of products.  A block is 32 consecutive elements along the row,
+ *   e = clamp(floor(log2(max |x|)) - 2, -127, 127)   the block's exponent, -127 where all are zero
+ *   c = x * 2^-e to the nearest of {0, 1/2, 1, 3/2, 2, 3, 4, 6} and their negatives, ties to the even mantissa, beyond 6: 6
+ *   x' = c * 2^e
+ * so |x - x'| <= 2^e where |x| < 6 * 2^e, and at most a quarter of |x| above (the block's largest only).  A block with an infinity or a NaN
+ * has the scale 255 and reads as NaN throughout.  Every step is exact or one IEEE operation: results are reproducible bit for bit.
+ *   codes   rows x (16 * blocks) bytes, blocks = ceil(cols / 32), the last block filled up with zeros; element 2j of a block in the
+ *           low half of its byte j, element 2j + 1 in the high half: sign, two bits exponent, one bit mantissa (E2M1)
+ *   scales  one byte e + 127 per block (E8M0, 255 = NaN), in tiles of 512 bytes for 128 rows x 4 blocks, the tiles of a band of 128 rows one
+ *           after the other: row r, block b at ((r / 128) * ceil(blocks / 4) + b / 4) * 512 + (r % 32) * 16 + (r % 128) / 32 * 4 + b % 4;
+ *           what stands behind the last row or block is 0
+ * Both 16-byte aligned.  These calls take no context: they keep nothing between calls and have no workspace, so calls on different
+ * streams and captured ones do not touch each other.  They run on the current device, which has to be that of their pointers.
+ * `type` is a zccl_type; ZCCL_E_ARG for null or misaligned pointers, an unknown type, a pitch below the row.  Zero rows or columns
+ * are allowed and write nothing.
+ */
+typedef enum { ZCCL_F32 = 0, ZCCL_BF16 = 1, ZCCL_F16 = 2 } zccl_type;
+size_t zccl_mx4_code_bytes(size_t rows, size_t cols);    /* pure host functions */
+size_t zccl_mx4_scale_bytes(size_t rows, size_t cols);
+/* x [device] rows x cols, `pitch` elements from row to row, aligned to its element.  transpose != 0: the form of x's transpose
+ * (cols x rows, blocks along x's columns), read without a copy. */
+int zccl_mx4_quantize(const void* x, int type, size_t rows, size_t cols, size_t pitch, int transpose, void* codes, void* scales, void* stream);
+/* y [device] rows x cols, `pitch` elements from row to row: every x', rounded once to `type`. */
+int zccl_mx4_dequantize(const void* codes, const void* scales, size_t rows, size_t cols, void* y, int type, size_t pitch, void* stream);
+
+/*
+ * What a data-parallel program does with the gradient that the ring has reduced: its norm over all tensors, and the AdamW
+ * step (decoupled weight decay) over all tensors at once.  No context, as for zccl_mx4_*.
+ *   g' = g * min(1, max_norm / (norm + 1e-6))  where norm is given, else g
+ *   m  = beta1 m + (1 - beta1) g'        v = beta2 v + (1 - beta2) g'^2
+ *   p  = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * in binary32, p rounded once to its type.  A norm that is negative or not finite leaves parameters, copies and states as they were.
+ *
+ * States in 32 bits are arrays of n floats.  In 8 bits m and r = sqrt(v) are held as E4M3 (n bytes each) with one scale byte e + 127 per
+ * block of 32 elements of the tensor (ceil(n / 32) bytes each), e the smallest power of two, from -127 on, at which the block's largest
+ * magnitude is at most 448 * 2^e; a block with a value that is not finite has the scale 255 and reads as NaN.  Rounding is stochastic
+ * (to nearest would leave a state that moves by less than half a step where it is: at beta2 = 0.999 most would never move): a value goes to the
+ * next one further from zero where its 16 random bits, in units of 1 / 65536 of a step, carry over.  r > 0 never becomes 0, which would
+ * leave m to be divided by eps alone.  The random bits are a function of `seed`, `step` and the element's place in the list, every
+ * tensor counted from a multiple of 32 on, so a step can be repeated bit for bit.
+ */
+typedef struct {
+    void* p;            /* [device] parameters, n elements of param_type */
+    const void* g;      /* [device] gradient, n elements of grad_type */
+    void* m;            /* [device] first moment: n floats, or n bytes */
+    void* v;            /* [device] second moment: n floats; or its root, n bytes */
+    void* m_scale;      /* [device] 8 bits: scales of m, ceil(n / 32) bytes; else not looked at */
+    void* v_scale;      /* [device] 8 bits: scales of the root */
+    void* copy;         /* [device] NULL, or receives the new parameters rounded to copy_type */
+    size_t n;
+} zccl_adamw_tensor;
+typedef struct {
+    int param_type, grad_type, copy_type;   /* zccl_type; a copy needs param_type ZCCL_F32 and is ZCCL_BF16 or ZCCL_F16 */
+    int state_bits;                         /* 32 or 8 */
+    double lr, beta1, beta2, eps, weight_decay;
+    long long step;                         /* from 1 on */
+    const long long* step_device;           /* [device] NULL, or where step is read when the call runs (for captured calls) */
+    const float* lr_device;                 /* [device] NULL, or where lr is read when the call runs */
+    unsigned long long seed;
+    const float* norm;                      /* [device] NULL, or the gradients' norm */
+    double max_norm;
+} zccl_adamw_config;
+/* Tensors [host, read before the call returns] may be any number and any size, 0 too; no two may overlap.  All pointers are aligned to their
+ * element.  ZCCL_E_ARG for what the host can see to be wrong; nothing has run then. */
+int zccl_adamw(const zccl_adamw_tensor* tensors, size_t count, const zccl_adamw_config* config, void* stream);
+/* norm [device] <- sqrt(sum of g^2) over `count` gradients of one type: g [host] device pointers, n [host] their lengths.  Sums of a fixed order in
+ * binary64, squares that leave the range of binary32 included: the same gradients on the same kind of GPU give the same bits.  `work` [device, 8-byte aligned] zccl_grad_norm_work(count) bytes,
+ * contents of no matter; calls that may run at the same time need one each. */
+size_t zccl_grad_norm_work(size_t count);   /* pure host function */
+int zccl_grad_norm(const void* const* g, const size_t* n, size_t count, int grad_type, float* norm, void* work, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

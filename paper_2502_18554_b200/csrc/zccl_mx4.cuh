@@ -1,0 +1,85 @@
+// Microscaled 4-bit floating point: the arithmetic of a block and the layout of the scales.  Not installed.
+#pragma once
+#include "zccl_device.cuh"
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+namespace zccl {
+
+constexpr int kMxBlock = 32;              // elements that share a scale
+constexpr int kMxGroup = 4 * kMxBlock;    // elements of a row that a tile of scales covers
+constexpr int kMxBand = 128;              // rows that a tile of scales covers
+constexpr int kMxTileBytes = 512;
+constexpr size_t kMxMaxGroups = 0x7FFFFFFFu;   // (row, group) pairs are counted in 32 bits: 2^38 elements
+
+__host__ __device__ inline size_t mx_blocks(size_t cols) { return (cols + kMxBlock - 1) / kMxBlock; }
+__host__ __device__ inline size_t mx_groups(size_t cols) { return (cols + kMxGroup - 1) / kMxGroup; }
+__host__ __device__ inline size_t mx_bands(size_t rows) { return (rows + kMxBand - 1) / kMxBand; }
+
+namespace {
+
+// Where the four scales of group g of row r begin.
+__device__ __forceinline__ size_t mx_scale_at(uint32_t r, uint32_t g, uint32_t groups)
+{
+    return ((size_t)(r >> 7) * groups + g) * kMxTileBytes + (r & 31u) * 16u + ((r >> 5) & 3u) * 4u;
+}
+
+__device__ __forceinline__ float mx_float(float v) { return v; }
+__device__ __forceinline__ float mx_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float mx_float(__half v) { return __half2float(v); }
+template <class T> __device__ __forceinline__ T mx_round(float v);
+template <> __device__ __forceinline__ float mx_round<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 mx_round<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half mx_round<__half>(float v) { return __float2half_rn(v); }
+
+// 4 or 8 values of a vector load, in binary32.
+template <class T> struct MxPack { T v[16 / sizeof(T)]; };
+
+// The biased exponent of a block whose largest magnitude has the bits `top`: floor(log2) is the exponent field, and a field
+// below 2 (e below -127, subnormal numbers and zero among them) ends at 0.  255 where `top` is no finite number.
+__device__ __forceinline__ uint32_t mx_exponent(uint32_t top)
+{
+    const uint32_t field = top >> 23;
+    return field == 255u ? 255u : field < 2u ? 0u : field - 2u;
+}
+// 2^-e, exact: 254 - s is a normal number's field for every finite s <= 252.  0 for a block of NaN, whose codes are zeros.
+__device__ __forceinline__ float mx_inverse(uint32_t s) { return __uint_as_float(s == 255u ? 0u : (254u - s) << 23); }
+// 2^e; e = -127 is a subnormal number
+__device__ __forceinline__ float mx_scale(uint32_t s) { return __uint_as_float(s == 0u ? 0x00400000u : s == 255u ? 0x7FC00000u : s << 23); }
+
+// Eight values of a block times 2^-e as eight codes (the conversion rounds to nearest, ties to even, and ends at 6).
+__device__ __forceinline__ uint32_t mx_encode8(const float (&v)[8], float inverse)
+{
+    uint32_t w;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(w)
+        : "f"(v[0] * inverse), "f"(v[1] * inverse), "f"(v[2] * inverse), "f"(v[3] * inverse),
+          "f"(v[4] * inverse), "f"(v[5] * inverse), "f"(v[6] * inverse), "f"(v[7] * inverse));
+    return w;
+}
+__device__ __forceinline__ void mx_decode8(uint32_t w, float scale, float (&v)[8])
+{
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "mov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+        v[2 * i] = f.x * scale;
+        v[2 * i + 1] = f.y * scale;
+    }
+}
+
+}  // namespace
+}  // namespace zccl
