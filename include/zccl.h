@@ -431,6 +431,16 @@ size_t zccl_mx4_scale_bytes(size_t rows, size_t cols);
 int zccl_mx4_quantize(const void* x, int type, size_t rows, size_t cols, size_t pitch, int transpose, void* codes, void* scales, void* stream);
 /* y [device] rows x cols, `pitch` elements from row to row: every x', rounded once to `type`. */
 int zccl_mx4_dequantize(const void* codes, const void* scales, size_t rows, size_t cols, void* y, int type, size_t pitch, void* stream);
+/*
+ * Product of two operands in this form: y [device, m x n, `pitch` elements from row to row] <- A B^T, A m x k, B n x k, both quantised along
+ * k: sums of exact products in binary32 on the tensor cores, each rounded once to `type`.  What is behind the last row and block of the scales
+ * has to be 0, as zccl_mx4_quantize leaves it.  The order of the sum depends on the sizes alone: the same call gives the same bits.  k = 0 gives
+ * zeros.  Waits inside the kernels are bounded; one that ran out leaves y unspecified and is recorded for zccl_mx4_status, which
+ * synchronises `stream`, returns ZCCL_OK or ZCCL_E_TIMEOUT for the current device and clears the record.
+ */
+int zccl_mx4_matmul(const void* a_codes, const void* a_scales, size_t m, const void* b_codes, const void* b_scales, size_t n, size_t k,
+                    void* y, int type, size_t pitch, void* stream);
+int zccl_mx4_status(void* stream);
 
 /*
  * What a data-parallel program does with the gradient that the ring has reduced: its norm over all tensors, and the AdamW

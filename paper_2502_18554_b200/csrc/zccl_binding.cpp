@@ -365,6 +365,23 @@ PyObject* mx4_dequantize(PyObject*, Args a, Py_ssize_t na)
     return status_on(*y, [&] { return zccl_mx4_dequantize(codes, scales, rows, cols, y->data_ptr(), type, pitch, st); });
 }
 
+// (a_codes, a_scales, b_codes, b_scales, k, y, stream)
+PyObject* mx4_matmul(PyObject*, Args a, Py_ssize_t na)
+{
+    if (!nargs_are(na, 7)) return nullptr;
+    const size_t k = PyLong_AsSize_t(a[4]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::Tensor* y;
+    int type;
+    size_t pitch;
+    void *ac, *as, *bc, *bs, *st;
+    if (!matrix(a[5], &y, &type, &pitch)) return nullptr;
+    const size_t m = y->size(0), n = y->size(1);
+    if (!bytes_of(a[0], zccl_mx4_code_bytes(m, k), *y, &ac) || !bytes_of(a[1], zccl_mx4_scale_bytes(m, k), *y, &as) || !bytes_of(a[2], zccl_mx4_code_bytes(n, k), *y, &bc) ||
+        !bytes_of(a[3], zccl_mx4_scale_bytes(n, k), *y, &bs) || !stream_on(a[6], *y, &st)) return nullptr;
+    return status_on(*y, [&] { return zccl_mx4_matmul(ac, as, m, bc, bs, n, k, y->data_ptr(), type, pitch, st); });
+}
+
 // A list or tuple of tensors, kept alive by its caller.
 struct Tensors {
     PyObject* seq = nullptr;
@@ -533,7 +550,7 @@ PyMethodDef methods[] = {
     FAST(compress), FAST(decompress), FAST(hop), FAST(compress_f64), FAST(decompress_f64), FAST(compress_tiled), FAST(decompress_tiled), FAST(sim_allreduce),
     {"sim_allgather", (PyCFunction)(void (*)(void))sim<zccl_sim_allgather>, METH_FASTCALL, nullptr},
     {"sim_reduce_scatter", (PyCFunction)(void (*)(void))sim<zccl_sim_reduce_scatter>, METH_FASTCALL, nullptr},
-    FAST(mx4_sizes), FAST(mx4_quantize), FAST(mx4_dequantize), FAST(adamw), FAST(grad_norm),
+    FAST(mx4_sizes), FAST(mx4_quantize), FAST(mx4_dequantize), FAST(mx4_matmul), FAST(adamw), FAST(grad_norm),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_zccl", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

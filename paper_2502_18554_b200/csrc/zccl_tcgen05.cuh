@@ -1,0 +1,112 @@
+// Inline PTX of the fifth-generation tensor cores, as the product of microscaled operands uses it.  Not installed.
+#pragma once
+#include "zccl_device.cuh"
+
+namespace zccl {
+namespace {
+
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+__device__ __forceinline__ void tmem_alloc(uint32_t* at_shared, uint32_t columns)
+{
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(at_shared)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_free(uint32_t at, uint32_t columns)
+{
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns));
+}
+__device__ __forceinline__ void tcgen05_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tcgen05_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// The barrier gets one arrival when everything that this thread has issued so far is done.
+__device__ __forceinline__ void tcgen05_commit(unsigned long long* bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+// 32 rows of 16 bytes from shared memory to four columns, once for each quarter of the lanes.
+__device__ __forceinline__ void tcgen05_copy_scales(uint32_t column, unsigned long long descriptor)
+{
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(column), "l"(descriptor) : "memory");
+}
+__device__ __forceinline__ void tcgen05_mma_mx4(uint32_t d, unsigned long long a, unsigned long long b, uint32_t instruction, uint32_t a_scale, uint32_t b_scale, bool add)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(instruction), "r"(a_scale), "r"(b_scale), "r"((uint32_t)add) : "memory");
+}
+// 32 columns of the warp's quarter of the lanes: a thread gets its lane's 32 values.
+__device__ __forceinline__ void tcgen05_load32(uint32_t at, uint32_t (&v)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+          "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+          "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(at));
+}
+__device__ __forceinline__ void tcgen05_load16(uint32_t at, uint32_t (&v)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(at));
+}
+__device__ __forceinline__ void tcgen05_wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// Operand tiles in shared memory: rows of 128 bytes, 128-byte swizzle, groups of eight rows 1024 bytes apart.
+__device__ __forceinline__ unsigned long long operand_descriptor(uint32_t at)
+{
+    return (unsigned long long)((at & 0x3FFFFu) >> 4) | 1ull << 16 | (unsigned long long)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// A tile of scales: 32 rows of 16 bytes, no swizzle, groups of eight rows 128 bytes apart.
+__device__ __forceinline__ unsigned long long scales_descriptor(uint32_t at)
+{
+    return (unsigned long long)((at & 0x3FFFFu) >> 4) | 1ull << 16 | (unsigned long long)(128 >> 4) << 32 | 1ull << 46;
+}
+// Instruction descriptor of kind::mxf4: E2M1 operands, E8M0 scales, both K-major, `n` columns; `id`: which pair of a word's
+// four scales the 64 elements of this instruction take (0 or 2).
+__host__ __device__ constexpr uint32_t mx4_instruction(uint32_t rows, uint32_t n, uint32_t id)
+{
+    return id << 4 | 1u << 7 | 1u << 10 | (n >> 3) << 17 | 1u << 23 | (rows >> 4) << 24 | id << 29;
+}
+
+__device__ __forceinline__ void tile_load(void* dst, const void* map, int x, int y, unsigned long long* bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void bytes_load(void* dst, const void* src, uint32_t bytes, unsigned long long* bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// A word of the shared memory of the cluster's CTA `rank`, at the address `at` of this one's.
+__device__ __forceinline__ float peer_load(uint32_t at, uint32_t rank)
+{
+    float v;
+    asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}" : "=f"(v) : "r"(at), "r"(rank) : "memory");
+    return v;
+}
+
+}  // namespace
+}  // namespace zccl

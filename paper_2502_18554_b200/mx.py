@@ -65,3 +65,58 @@ def dequantize(q: Mx4, dtype: torch.dtype = torch.float32, out: torch.Tensor | N
         raise ValueError(f"expected an output [{q.rows}, {q.cols}], got {list(out.shape)}")
     z._check(z.native().mx4_dequantize(q.codes, q.scales, out, stream), "zccl_mx4_dequantize")
     return out
+
+
+def matmul(a: Mx4, b: Mx4, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """A B^T of two operands that are quantised along the contraction: a [m, k] and b [n, k] to [m, n], sums in binary32, each
+    rounded once to `dtype` (float32, bfloat16 or float16)."""
+    if a.cols != b.cols:
+        raise ValueError(f"operands are contracted over {a.cols} and {b.cols} elements")
+    if out is None:
+        with _allocating(stream):
+            out = torch.empty(a.rows, b.rows, dtype=dtype, device=a.codes.device)
+    elif tuple(out.shape) != (a.rows, b.rows):
+        raise ValueError(f"expected an output [{a.rows}, {b.rows}], got {list(out.shape)}")
+    z._check(z.native().mx4_matmul(a.codes, a.scales, b.codes, b.scales, a.cols, out, stream), "zccl_mx4_matmul")
+    return out
+
+
+def status(stream=None) -> int:
+    """zccl_mx4_status of the current device: waits for `stream`; z.OK or z.E_TIMEOUT."""
+    return int(z.lib().zccl_mx4_status(z._stream_ptr(stream)))
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w):
+        ctx.save_for_backward(x, w)
+        return matmul(quantize(x), quantize(w), x.dtype)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, w = ctx.saved_tensors
+        return linear_backward(dy.contiguous(), x, w, ctx.needs_input_grad)
+
+
+def linear(x: torch.Tensor, w: torch.Tensor | Mx4) -> torch.Tensor:
+    """x W^T with both sides in microscaled form, in x's type.  x is [..., k]; `w` is [n, k], or already quantised (weights that
+    are laid out once; no gradient then).  With a tensor for `w` this is differentiable, by linear_backward."""
+    rows = x.reshape(-1, x.shape[-1])
+    if isinstance(w, Mx4):
+        if torch.is_grad_enabled() and x.requires_grad:
+            raise ValueError("quantised weights are for inference: pass the weights themselves to train, or detach x")
+        y = matmul(quantize(rows), w, x.dtype)
+    else:
+        if w.dtype != x.dtype:
+            raise ValueError(f"x is {x.dtype}, the weights are {w.dtype}")
+        y = _Linear.apply(rows, w)
+    return y.view(*x.shape[:-1], y.shape[-1])
+
+
+def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, needed=(True, True)):
+    """The gradients of linear(x, w) for matrices, from dy [m, n]: dx = Q(dy) Q(w^T)^T, contracted and quantised along n, and
+    dw = Q(dy^T) Q(x^T)^T along m, each in its operand's type (quantisation itself passes gradients on unchanged)."""
+    dx = matmul(quantize(dy), quantize(w, transpose=True), x.dtype) if needed[0] else None
+    dw = matmul(quantize(dy, transpose=True), quantize(x, transpose=True), w.dtype) if needed[1] else None
+    return dx, dw
