@@ -4,6 +4,7 @@
 // (3.3 us of it the look-up of the current stream), here it takes 0.4 us.  The calls themselves are the C boundary's.
 #include <Python.h>
 
+#include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
@@ -327,6 +328,75 @@ PyObject* status_on(const at::Tensor& t, F&& f)
     }
 }
 
+// ---- microscaled 4-bit floating point.  Outputs are allocated here, on the stream that the call runs on: through Python the small
+// allocations of a call took longer than its kernels.
+
+// The device and stream of a call, current for its duration.
+struct Place {
+    c10::cuda::OptionalCUDAStreamGuard guard;
+    void* st = nullptr;
+    bool take(PyObject* stream, const at::Tensor& t)
+    {
+        if (!stream_on(stream, t, &st)) return false;
+        guard.reset_stream(c10::cuda::getStreamFromExternal((cudaStream_t)st, t.device().index()));
+        return true;
+    }
+};
+// Runs what allocates or launches; C++ exceptions end here.
+template <class F>
+PyObject* guarded(F&& f)
+{
+    try {
+        return f();
+    } catch (const std::exception& e) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+at::Tensor new_bytes(size_t n, const at::Tensor& like) { return at::empty({(int64_t)n}, like.options().dtype(at::kByte)); }
+struct Form {
+    at::Tensor codes, scales;
+};
+Form new_form(size_t rows, size_t cols, const at::Tensor& like) { return {new_bytes(zccl_mx4_code_bytes(rows, cols), like), new_bytes(zccl_mx4_scale_bytes(rows, cols), like)}; }
+
+struct Matrix {
+    const at::Tensor* t = nullptr;
+    int type = 0;
+    size_t pitch = 0, rows = 0, cols = 0;
+    bool take(PyObject* o)
+    {
+        if (!matrix(o, &t, &type, &pitch)) return false;
+        rows = (size_t)t->size(0);
+        cols = (size_t)t->size(1);
+        return true;
+    }
+    int quantize(bool transpose, const Form& f, void* st) const
+    {
+        return zccl_mx4_quantize(t->data_ptr(), type, rows, cols, pitch, transpose, f.codes.data_ptr(), f.scales.data_ptr(), st);
+    }
+};
+int multiply(const Form& a, size_t m, const Form& b, size_t n, size_t k, const at::Tensor& y, void* st)
+{
+    return zccl_mx4_matmul(a.codes.data_ptr(), a.scales.data_ptr(), m, b.codes.data_ptr(), b.scales.data_ptr(), n, k, y.data_ptr(), type_of(y), n, st);
+}
+// A form that the caller has: bytes of the right number on the right device.
+bool take_form(PyObject* codes, PyObject* scales, size_t rows, size_t cols, const at::Tensor& like, Form* f)
+{
+    void* p;
+    if (!bytes_of(codes, zccl_mx4_code_bytes(rows, cols), like, &p) || !bytes_of(scales, zccl_mx4_scale_bytes(rows, cols), like, &p)) return false;
+    f->codes = THPVariable_Unpack(codes);
+    f->scales = THPVariable_Unpack(scales);
+    return true;
+}
+bool element_type(PyObject* o, c10::ScalarType* dt)
+{
+    if (!THPDtype_Check(o)) return refuse("expected a dtype");
+    *dt = ((THPDtype*)o)->scalar_type;
+    return *dt == c10::kFloat || *dt == c10::kBFloat16 || *dt == c10::kHalf || refuse("expected float32, bfloat16 or float16");
+}
+PyObject* wrapped(int rc, const at::Tensor& t) { return rc == ZCCL_OK ? THPVariable_Wrap(t) : PyLong_FromLong(rc); }
+
 // (rows, cols) -> bytes of codes and of scales
 PyObject* mx4_sizes(PyObject*, Args a, Py_ssize_t na)
 {
@@ -336,50 +406,142 @@ PyObject* mx4_sizes(PyObject*, Args a, Py_ssize_t na)
     return Py_BuildValue("nn", (Py_ssize_t)zccl_mx4_code_bytes(rows, cols), (Py_ssize_t)zccl_mx4_scale_bytes(rows, cols));
 }
 
-// (x, transpose, codes, scales, stream)
+// (x, transpose, codes or None, scales or None, stream) -> (codes, scales) or a status
 PyObject* mx4_quantize(PyObject*, Args a, Py_ssize_t na)
 {
     if (!nargs_are(na, 5)) return nullptr;
-    const at::Tensor* x;
-    int type;
-    size_t pitch;
-    void *codes, *scales, *st;
-    if (!matrix(a[0], &x, &type, &pitch)) return nullptr;
-    const int transpose = PyObject_IsTrue(a[1]);
-    const size_t rows = x->size(0), cols = x->size(1), r = transpose ? cols : rows, c = transpose ? rows : cols;
-    if (!bytes_of(a[2], zccl_mx4_code_bytes(r, c), *x, &codes) || !bytes_of(a[3], zccl_mx4_scale_bytes(r, c), *x, &scales) || !stream_on(a[4], *x, &st)) return nullptr;
-    return status_on(*x, [&] { return zccl_mx4_quantize(x->data_ptr(), type, rows, cols, pitch, transpose, codes, scales, st); });
+    Matrix x;
+    if (!x.take(a[0])) return nullptr;
+    const bool transpose = PyObject_IsTrue(a[1]) == 1;
+    const size_t rows = transpose ? x.cols : x.rows, cols = transpose ? x.rows : x.cols;
+    Form f;
+    const bool given = a[2] != Py_None;
+    if (given && !take_form(a[2], a[3], rows, cols, *x.t, &f)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        Place place;
+        if (!place.take(a[4], *x.t)) return nullptr;
+        if (!given) f = new_form(rows, cols, *x.t);
+        const int rc = x.quantize(transpose, f, place.st);
+        if (rc != ZCCL_OK) return PyLong_FromLong(rc);
+        return Py_BuildValue("NN", THPVariable_Wrap(f.codes), THPVariable_Wrap(f.scales));
+    });
 }
 
-// (codes, scales, y, stream)
+// (codes, scales, rows, cols, dtype, y or None, stream) -> y or a status
 PyObject* mx4_dequantize(PyObject*, Args a, Py_ssize_t na)
 {
-    if (!nargs_are(na, 4)) return nullptr;
-    const at::Tensor* y;
-    int type;
-    size_t pitch;
-    void *codes, *scales, *st;
-    if (!matrix(a[2], &y, &type, &pitch)) return nullptr;
-    const size_t rows = y->size(0), cols = y->size(1);
-    if (!bytes_of(a[0], zccl_mx4_code_bytes(rows, cols), *y, &codes) || !bytes_of(a[1], zccl_mx4_scale_bytes(rows, cols), *y, &scales) || !stream_on(a[3], *y, &st)) return nullptr;
-    return status_on(*y, [&] { return zccl_mx4_dequantize(codes, scales, rows, cols, y->data_ptr(), type, pitch, st); });
+    if (!nargs_are(na, 7)) return nullptr;
+    const at::Tensor* codes;
+    Form f;
+    const size_t rows = PyLong_AsSize_t(a[2]), cols = PyLong_AsSize_t(a[3]);
+    if (PyErr_Occurred() || !cuda_tensor(a[0], &codes) || !take_form(a[0], a[1], rows, cols, *codes, &f)) return nullptr;
+    Matrix y;
+    c10::ScalarType dt = c10::kFloat;
+    const bool given = a[5] != Py_None;
+    if (given) {
+        if (!y.take(a[5])) return nullptr;
+        if (y.rows != rows || y.cols != cols || y.t->device() != codes->device()) return refuse("the output is of another size or device than the form"), nullptr;
+    } else if (!element_type(a[4], &dt)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        Place place;
+        if (!place.take(a[6], *codes)) return nullptr;
+        const at::Tensor out = given ? *y.t : at::empty({(int64_t)rows, (int64_t)cols}, codes->options().dtype(dt));
+        return wrapped(zccl_mx4_dequantize(f.codes.data_ptr(), f.scales.data_ptr(), rows, cols, out.data_ptr(), type_of(out), given ? y.pitch : cols, place.st), out);
+    });
 }
 
-// (a_codes, a_scales, b_codes, b_scales, k, y, stream)
+// (a_codes, a_scales, m, b_codes, b_scales, n, k, dtype, y or None, stream) -> y or a status
 PyObject* mx4_matmul(PyObject*, Args a, Py_ssize_t na)
 {
-    if (!nargs_are(na, 7)) return nullptr;
-    const size_t k = PyLong_AsSize_t(a[4]);
-    if (PyErr_Occurred()) return nullptr;
-    const at::Tensor* y;
-    int type;
-    size_t pitch;
-    void *ac, *as, *bc, *bs, *st;
-    if (!matrix(a[5], &y, &type, &pitch)) return nullptr;
-    const size_t m = y->size(0), n = y->size(1);
-    if (!bytes_of(a[0], zccl_mx4_code_bytes(m, k), *y, &ac) || !bytes_of(a[1], zccl_mx4_scale_bytes(m, k), *y, &as) || !bytes_of(a[2], zccl_mx4_code_bytes(n, k), *y, &bc) ||
-        !bytes_of(a[3], zccl_mx4_scale_bytes(n, k), *y, &bs) || !stream_on(a[6], *y, &st)) return nullptr;
-    return status_on(*y, [&] { return zccl_mx4_matmul(ac, as, m, bc, bs, n, k, y->data_ptr(), type, pitch, st); });
+    if (!nargs_are(na, 10)) return nullptr;
+    const size_t m = PyLong_AsSize_t(a[2]), n = PyLong_AsSize_t(a[5]), k = PyLong_AsSize_t(a[6]);
+    const at::Tensor* codes;
+    Form l, r;
+    if (PyErr_Occurred() || !cuda_tensor(a[0], &codes) || !take_form(a[0], a[1], m, k, *codes, &l) || !take_form(a[3], a[4], n, k, *codes, &r)) return nullptr;
+    Matrix y;
+    c10::ScalarType dt = c10::kFloat;
+    const bool given = a[8] != Py_None;
+    if (given) {
+        if (!y.take(a[8])) return nullptr;
+        if (y.rows != m || y.cols != n || y.t->device() != codes->device()) return refuse("the output is of another size or device than the operands"), nullptr;
+    } else if (!element_type(a[7], &dt)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        Place place;
+        if (!place.take(a[9], *codes)) return nullptr;
+        const at::Tensor out = given ? *y.t : at::empty({(int64_t)m, (int64_t)n}, codes->options().dtype(dt));
+        return wrapped(zccl_mx4_matmul(l.codes.data_ptr(), l.scales.data_ptr(), m, r.codes.data_ptr(), r.scales.data_ptr(), n, k, out.data_ptr(), type_of(out), given ? y.pitch : n, place.st), out);
+    });
+}
+
+// (x, w) or (x, codes, scales, n) -> x W^T in x's type, or a status
+PyObject* mx4_linear(PyObject*, Args a, Py_ssize_t na)
+{
+    if (na != 2 && !nargs_are(na, 4)) return nullptr;
+    Matrix x, w;
+    Form held;
+    size_t n = 0;
+    if (!x.take(a[0])) return nullptr;
+    if (na == 2) {
+        if (!w.take(a[1])) return nullptr;
+        if (w.cols != x.cols || w.type != x.type || w.t->device() != x.t->device()) return refuse("x and the weights differ in type, device or the length of their rows"), nullptr;
+        n = w.rows;
+    } else {
+        n = PyLong_AsSize_t(a[3]);
+        if (PyErr_Occurred() || !take_form(a[1], a[2], n, x.cols, *x.t, &held)) return nullptr;
+    }
+    return guarded([&]() -> PyObject* {
+        Place place;
+        if (!place.take(Py_None, *x.t)) return nullptr;
+        const Form f = new_form(x.rows, x.cols, *x.t);
+        const at::Tensor y = at::empty({(int64_t)x.rows, (int64_t)n}, x.t->options());
+        int rc = x.quantize(false, f, place.st);
+        if (rc == ZCCL_OK && na == 2) {
+            held = new_form(n, x.cols, *x.t);
+            rc = w.quantize(false, held, place.st);
+        }
+        if (rc == ZCCL_OK) rc = multiply(f, x.rows, held, n, x.cols, y, place.st);
+        return wrapped(rc, y);
+    });
+}
+
+// (dy, x, w, dx wanted, dw wanted) -> (dx or None, dw or None), or a status
+PyObject* mx4_linear_backward(PyObject*, Args a, Py_ssize_t na)
+{
+    if (!nargs_are(na, 5)) return nullptr;
+    Matrix dy, x, w;
+    if (!dy.take(a[0]) || !x.take(a[1]) || !w.take(a[2])) return nullptr;
+    const size_t m = x.rows, k = x.cols, n = w.rows;
+    if (dy.rows != m || dy.cols != n || w.cols != k) return refuse("sizes of the gradient, the input and the weights do not belong together"), nullptr;
+    if (dy.t->device() != x.t->device() || w.t->device() != x.t->device()) return refuse("all tensors of a call are on one device"), nullptr;
+    const bool want_x = PyObject_IsTrue(a[3]) == 1, want_w = PyObject_IsTrue(a[4]) == 1;
+    return guarded([&]() -> PyObject* {
+        Place place;
+        if (!place.take(Py_None, *x.t)) return nullptr;
+        at::Tensor dx, dw;
+        int rc = ZCCL_OK;
+        if (want_x) {
+            const Form l = new_form(m, n, *x.t), r = new_form(k, n, *x.t);
+            dx = at::empty({(int64_t)m, (int64_t)k}, x.t->options());
+            rc = dy.quantize(false, l, place.st);
+            if (rc == ZCCL_OK) rc = w.quantize(true, r, place.st);
+            if (rc == ZCCL_OK) rc = multiply(l, m, r, k, n, dx, place.st);
+        }
+        if (want_w && rc == ZCCL_OK) {
+            const Form l = new_form(n, m, *x.t), r = new_form(k, m, *x.t);
+            dw = at::empty({(int64_t)n, (int64_t)k}, w.t->options());
+            rc = dy.quantize(true, l, place.st);
+            if (rc == ZCCL_OK) rc = x.quantize(true, r, place.st);
+            if (rc == ZCCL_OK) rc = multiply(l, n, r, k, m, dw, place.st);
+        }
+        if (rc != ZCCL_OK) return PyLong_FromLong(rc);
+        Py_INCREF(Py_None);
+        Py_INCREF(Py_None);
+        PyObject* const ox = want_x ? THPVariable_Wrap(dx) : Py_None;
+        PyObject* const ow = want_w ? THPVariable_Wrap(dw) : Py_None;
+        if (want_x) Py_DECREF(Py_None);
+        if (want_w) Py_DECREF(Py_None);
+        return Py_BuildValue("NN", ox, ow);
+    });
 }
 
 // A list or tuple of tensors, kept alive by its caller.
@@ -513,35 +675,35 @@ PyObject* adamw(PyObject*, Args a, Py_ssize_t na)
     return rc;
 }
 
-// (grads, norm, work, stream)
+// (grads, norm or None, stream) -> norm or a status
 PyObject* grad_norm(PyObject*, Args a, Py_ssize_t na)
 {
-    if (!nargs_are(na, 4)) return nullptr;
+    if (!nargs_are(na, 3)) return nullptr;
     Tensors g;
-    const at::Tensor *norm, *work, *t;
-    if (!g.take(a[0]) || !cuda_tensor(a[1], &norm) || !cuda_tensor(a[2], &work)) return nullptr;
+    const at::Tensor *norm = nullptr, *first = nullptr, *t;
+    const bool given = a[1] != Py_None;
+    if (!g.take(a[0]) || (given && !cuda_tensor(a[1], &norm))) return nullptr;
     const size_t count = g.count();
-    if (norm->scalar_type() != c10::kFloat || norm->numel() != 1) return refuse("the norm is one float32"), nullptr;
-    if (work->scalar_type() != c10::kByte || !work->is_contiguous() || (size_t)work->numel() < zccl_grad_norm_work(count) || work->device() != norm->device())
-        return refuse("the workspace is contiguous uint8, of grad_norm_work(count) bytes at least, on the norm's device"), nullptr;
+    if (given && (norm->scalar_type() != c10::kFloat || norm->numel() != 1)) return refuse("the norm is one float32"), nullptr;
+    if (count && !g.at(0, &first)) return nullptr;
+    if (!given && !count) return refuse("no gradients to take a device from: pass an output"), nullptr;
+    const at::Tensor& like = given ? *norm : *first;
+    const int type = first ? type_of(*first) : ZCCL_F32;
+    if (type < 0) return refuse("expected float32, bfloat16 or float16"), nullptr;
     std::vector<const void*> at(count);
     std::vector<size_t> n(count);
-    int type = ZCCL_F32;
-    const at::Tensor* first = nullptr;
     for (size_t i = 0; i < count; ++i) {
-        if (!g.at(i, &t)) return nullptr;
-        if (!first) {
-            first = t;
-            type = type_of(*t);
-            if (type < 0) return refuse("expected float32, bfloat16 or float16"), nullptr;
-        }
-        if (!entry(g, i, first->scalar_type(), (size_t)t->numel(), *norm, &t)) return nullptr;
+        if (!g.at(i, &t) || !entry(g, i, first->scalar_type(), (size_t)t->numel(), like, &t)) return nullptr;
         at[i] = t->data_ptr();
         n[i] = (size_t)t->numel();
     }
-    void* st;
-    if (!stream_on(a[3], *norm, &st)) return nullptr;
-    return status_on(*norm, [&] { return zccl_grad_norm(at.data(), n.data(), count, type, (float*)norm->data_ptr(), work->data_ptr(), st); });
+    return guarded([&]() -> PyObject* {
+        Place place;
+        if (!place.take(a[2], like)) return nullptr;
+        const at::Tensor out = given ? *norm : at::empty({1}, like.options().dtype(c10::kFloat));
+        const at::Tensor work = new_bytes(zccl_grad_norm_work(count), like);
+        return wrapped(zccl_grad_norm(at.data(), n.data(), count, type, (float*)out.data_ptr(), work.data_ptr(), place.st), out);
+    });
 }
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
@@ -550,7 +712,7 @@ PyMethodDef methods[] = {
     FAST(compress), FAST(decompress), FAST(hop), FAST(compress_f64), FAST(decompress_f64), FAST(compress_tiled), FAST(decompress_tiled), FAST(sim_allreduce),
     {"sim_allgather", (PyCFunction)(void (*)(void))sim<zccl_sim_allgather>, METH_FASTCALL, nullptr},
     {"sim_reduce_scatter", (PyCFunction)(void (*)(void))sim<zccl_sim_reduce_scatter>, METH_FASTCALL, nullptr},
-    FAST(mx4_sizes), FAST(mx4_quantize), FAST(mx4_dequantize), FAST(mx4_matmul), FAST(adamw), FAST(grad_norm),
+    FAST(mx4_sizes), FAST(mx4_quantize), FAST(mx4_dequantize), FAST(mx4_matmul), FAST(mx4_linear), FAST(mx4_linear_backward), FAST(adamw), FAST(grad_norm),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_zccl", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -9,183 +9,285 @@ namespace {
 
 constexpr int kMxThreads = 256;
 
-// Eight neighbouring elements of a row, in binary32; what lies behind `cols` counts as zero.
-template <class T, bool VEC>
-__device__ __forceinline__ void load8(const T* __restrict__ row, uint32_t at, uint32_t cols, float (&v)[8])
+// Two elements of a 16-bit type in a word, or of binary32 in two.
+template <class T> struct MxTwo { uint32_t w; };
+template <> struct MxTwo<float> { float a, b; };
+
+// Largest magnitudes so far of the two places, as bits: magnitudes of floats are in the order of their bits, with infinity and
+// NaN at the top, so 16-bit types are compared as two halves of a word.
+template <class T> struct MxTop { uint32_t w = 0; };
+template <> struct MxTop<float> { uint32_t a = 0, b = 0; };
+template <class T>
+__device__ __forceinline__ void mx_top(MxTop<T>& top, const MxTwo<T>& v) { top.w = __vmaxu2(top.w, v.w & 0x7FFF7FFFu); }
+__device__ __forceinline__ void mx_top(MxTop<float>& top, const MxTwo<float>& v)
 {
-    constexpr int kPer = 16 / sizeof(T);
+    top.a = max(top.a, __float_as_uint(v.a) & 0x7FFFFFFFu);
+    top.b = max(top.b, __float_as_uint(v.b) & 0x7FFFFFFFu);
+}
+// The bits of a magnitude in binary32.
+template <class T> __device__ __forceinline__ uint32_t mx_bits(uint32_t half);
+template <> __device__ __forceinline__ uint32_t mx_bits<__nv_bfloat16>(uint32_t half) { return half << 16; }
+template <> __device__ __forceinline__ uint32_t mx_bits<__half>(uint32_t half) { return __float_as_uint(__half2float(__ushort_as_half((unsigned short)half))); }
+template <class T> __device__ __forceinline__ uint32_t mx_first(const MxTop<T>& top) { return mx_bits<T>(top.w & 0xFFFFu); }
+template <class T> __device__ __forceinline__ uint32_t mx_second(const MxTop<T>& top) { return mx_bits<T>(top.w >> 16); }
+__device__ __forceinline__ uint32_t mx_first(const MxTop<float>& top) { return top.a; }
+__device__ __forceinline__ uint32_t mx_second(const MxTop<float>& top) { return top.b; }
+
+// Both elements times their powers of two, exactly, as binary32.  bfloat16 has binary32's exponents, so there the product of two elements is
+// one instruction (what falls below its range is far below the smallest code's half).
+template <class T>
+__device__ __forceinline__ void mx_scaled(const MxTwo<T>& v, float first, float second, uint32_t, float& a, float& b)
+{
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v.w));
+    a = f.x * first;
+    b = f.y * second;
+}
+__device__ __forceinline__ void mx_scaled(const MxTwo<float>& v, float first, float second, uint32_t, float& a, float& b)
+{
+    a = v.a * first;
+    b = v.b * second;
+}
+__device__ __forceinline__ void mx_scaled(const MxTwo<__nv_bfloat16>& v, float, float, uint32_t both, float& a, float& b)
+{
+    const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&v.w), *reinterpret_cast<const __nv_bfloat162*>(&both));
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(&p);
+    a = __uint_as_float(w << 16);
+    b = __uint_as_float(w & 0xFFFF0000u);
+}
+// 2^-e of two places as a pair of bfloat16.
+__device__ __forceinline__ uint32_t mx_pair(float first, float second) { return __float_as_uint(first) >> 16 | (__float_as_uint(second) & 0xFFFF0000u); }
+
+// Eight neighbouring elements of a row; what lies behind `cols` counts as zero.
+template <class T, bool VEC>
+__device__ __forceinline__ void load8(const T* __restrict__ row, uint32_t at, uint32_t cols, MxTwo<T> (&v)[4])
+{
     if (VEC && at + 8 <= cols) {
 #pragma unroll
-        for (int i = 0; i < 8 / kPer; ++i) {
-            const uint4 raw = __ldcs(reinterpret_cast<const uint4*>(row + at) + i);
-            const MxPack<T> p = *reinterpret_cast<const MxPack<T>*>(&raw);
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) v[kPer * i + j] = mx_float(p.v[j]);
-        }
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(v)[i] = __ldcs(reinterpret_cast<const uint4*>(row + at) + i);
     } else {
+        T e[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = at + i < cols ? mx_float(row[at + i]) : 0.0f;
+        for (int i = 0; i < 8; ++i) e[i] = at + i < cols ? row[at + i] : mx_round<T>(0.0f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const MxTwo<T>*>(&e[2 * i]);
     }
 }
 
-__device__ __forceinline__ uint32_t top_of(const float (&v)[8])
-{
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    return top;
-}
-
-// Rows: 16 lanes take a group of 128 neighbouring elements (four blocks, one word of scales), a lane eight of them, so
-// loads are 16 bytes a lane and codes leave as whole lines.  Groups of the rows that fill the last band up, and blocks
-// behind the last, are quantised as zeros: only their scales are written.
-template <class T, bool VEC>
+// Rows: 16 lanes take STRIP groups of 128 neighbouring elements of a row (a group: four blocks, one word of scales), a lane
+// eight elements of each, so loads are 16 bytes a lane and codes leave as whole lines.  Groups of the rows that fill the last band
+// up, and blocks behind the last, are quantised as zeros: only their scales are written.
+// Bound by memory where it is large; with one group at a time the indexes cost more instructions than the elements (23 to an element, 52.5 us
+// for 8192 x 8192 bf16).
+template <class T, bool VEC, int STRIP>
 __global__ void __launch_bounds__(kMxThreads) mx_quantize_rows_kernel(const T* __restrict__ x, uint32_t rows, uint32_t cols, size_t pitch,
-                                                                       uint32_t blocks, uint32_t groups, uint32_t total, uint32_t step_row, uint32_t step_group,
-                                                                       uint32_t* __restrict__ codes, unsigned char* __restrict__ scales)
+                                                                       uint32_t blocks, uint32_t groups, uint32_t strips, uint32_t total, uint32_t step_row,
+                                                                       uint32_t step_strip, uint32_t* __restrict__ codes, unsigned char* __restrict__ scales)
 {
     pdl_enter();
     const uint32_t sub = threadIdx.x & 15u;
     uint32_t u = blockIdx.x * (kMxThreads / 16) + (threadIdx.x >> 4);
-    uint32_t r = u / groups, g = u - r * groups;
+    uint32_t r = u / strips, strip = u - r * strips;
     const uint32_t stride = gridDim.x * (kMxThreads / 16);
     // whole warps go round together: the last round's idle half takes part in the exchanges with zeros
     for (uint32_t first = u & ~1u; first < total; first += stride, u += stride) {
-        float v[8];
-        const uint32_t at = g * kMxGroup + sub * 8;
-        if (u < total && r < rows && at < cols) load8<T, VEC>(x + (size_t)r * pitch, at, cols, v);
-        else {
+        MxTwo<T> v[STRIP][4];
+        const uint32_t g0 = strip * STRIP, at = g0 * kMxGroup + sub * 8;
+        const T* const row = x + (size_t)r * pitch;
+        const bool there = u < total && r < rows;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-        }
-        uint32_t top = top_of(v);
-        top = max(top, __shfl_xor_sync(kFull, top, 1));
-        top = max(top, __shfl_xor_sync(kFull, top, 2));
-        const uint32_t s = mx_exponent(top);
-        const uint32_t w = s == 255u ? 0u : mx_encode8(v, mx_inverse(s));
-        uint32_t four = s << (8 * (sub >> 2));
-        four |= __shfl_xor_sync(kFull, four, 4);
-        four |= __shfl_xor_sync(kFull, four, 8);
-        if (u < total) {
-            if (r < rows && (at >> 5) < blocks) codes[((size_t)r * blocks + (at >> 5)) * 4 + (sub & 3u)] = w;
-            if (sub == 0) *reinterpret_cast<uint32_t*>(scales + mx_scale_at(r, g, groups)) = four;
-        }
-        r += step_row;
-        g += step_group;
-        if (g >= groups) { g -= groups; ++r; }
-    }
-}
-
-// Columns: the form of the transpose.  A warp takes 32 rows x 64 columns (a lane two columns, so a row's load is one line
-// of 16-bit elements), a CTA the four blocks of a word of scales.  A lane then holds whole blocks: no exchange, and a
-// block's codes leave as 16 bytes; the four warps' fill a sector pair of the same row of the output.
-template <class T, bool VEC>
-__global__ void __launch_bounds__(128) mx_quantize_columns_kernel(const T* __restrict__ x, uint32_t rows, uint32_t cols, size_t pitch, uint32_t blocks,
-                                                                   uint32_t groups, uint32_t across, uint4* __restrict__ codes, unsigned char* __restrict__ scales)
-{
-    pdl_enter();
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
-    const uint32_t g = blockIdx.x / across;
-    const uint32_t c = (blockIdx.x - g * across) * 64 + lane * 2;
-    const uint32_t b = g * 4 + warp;
-    const uint32_t r0 = b * kMxBlock;
-    __shared__ __align__(4) unsigned char sh[64][4];
-    uint32_t top0 = 0, top1 = 0;
-    T v0[kMxBlock], v1[kMxBlock];
-    const bool any = c < cols, both = c + 1 < cols;
+        for (int j = 0; j < STRIP; ++j) {
+            const uint32_t here = at + j * kMxGroup;
+            if (there && here < cols) load8<T, VEC>(row, here, cols, v[j]);
+            else {
 #pragma unroll
-    for (int i = 0; i < kMxBlock; ++i) {
-        const T* p = x + (size_t)(r0 + i) * pitch + c;
-        v0[i] = v1[i] = mx_round<T>(0.0f);
-        if (any && r0 + i < rows) {
-            if (VEC && both) {
-                struct alignas(2 * sizeof(T)) Two { T a, b; };
-                const Two two = *reinterpret_cast<const Two*>(p);
-                v0[i] = two.a;
-                v1[i] = two.b;
-            } else {
-                v0[i] = p[0];
-                if (both) v1[i] = p[1];
+                for (int i = 0; i < 4; ++i) v[j][i] = MxTwo<T>{};
             }
         }
-    }
+        uint32_t* const out = codes + ((size_t)r * blocks + (at >> 5)) * 4 + (sub & 3u);
+        unsigned char* const scale = scales + mx_scale_at(r, g0, groups);
 #pragma unroll
-    for (int i = 0; i < kMxBlock; ++i) {
-        top0 = max(top0, __float_as_uint(mx_float(v0[i])) & 0x7FFFFFFFu);
-        top1 = max(top1, __float_as_uint(mx_float(v1[i])) & 0x7FFFFFFFu);
-    }
+        for (int j = 0; j < STRIP; ++j) {
+            MxTop<T> two;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const uint32_t s = mx_exponent(j ? top1 : top0);
-        const float inverse = mx_inverse(s);
-        uint32_t w[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
+            for (int i = 0; i < 4; ++i) mx_top(two, v[j][i]);
+            uint32_t top = max(mx_first(two), mx_second(two));
+            top = max(top, __shfl_xor_sync(kFull, top, 1));
+            top = max(top, __shfl_xor_sync(kFull, top, 2));
+            const uint32_t s = mx_exponent(top);
+            const float inverse = mx_inverse(s);
+            const uint32_t both = mx_pair(inverse, inverse);
             float f[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = mx_float(j ? v1[8 * q + i] : v0[8 * q + i]);
-            w[q] = s == 255u ? 0u : mx_encode8(f, inverse);
+            for (int i = 0; i < 4; ++i) mx_scaled(v[j][i], inverse, inverse, both, f[2 * i], f[2 * i + 1]);
+            const uint32_t w = s == 255u ? 0u : mx_encode8(f);
+            uint32_t four = s << (8 * (sub >> 2));
+            four |= __shfl_xor_sync(kFull, four, 4);
+            four |= __shfl_xor_sync(kFull, four, 8);
+            if (there && (at >> 5) + 4 * j < blocks) out[16 * j] = w;
+            if (sub == 0 && u < total && g0 + j < groups) *reinterpret_cast<uint32_t*>(scale + j * kMxTileBytes) = four;
         }
-        if (c + j < cols && b < blocks) codes[(size_t)(c + j) * blocks + b] = make_uint4(w[0], w[1], w[2], w[3]);
-        sh[lane * 2 + j][warp] = (unsigned char)s;
-    }
-    __syncthreads();
-    if (threadIdx.x < 64) {
-        const uint32_t column = (blockIdx.x - g * across) * 64 + threadIdx.x;
-        *reinterpret_cast<uint32_t*>(scales + mx_scale_at(column, g, groups)) = *reinterpret_cast<const uint32_t*>(sh[threadIdx.x]);
+        r += step_row;
+        strip += step_strip;
+        if (strip >= strips) { strip -= strips; ++r; }
     }
 }
 
+// Columns: the form of the transpose.  A warp takes a block of 32 rows x 64 columns (a lane two columns, so a row's load is one line
+// of 16-bit elements): a lane holds whole blocks and needs no exchange.  A CTA's eight blocks go through shared memory, so that they leave as lines of
+// 128 bytes and words of scales.
+constexpr int kColumnWarps = 8, kColumnWidth = 64;
+constexpr int kColumnPad = kColumnWarps + 1;   // sixteen-byte pieces of a column in shared memory: an odd number keeps the writes of eight lanes apart
 template <class T, bool VEC>
+__global__ void __launch_bounds__(kColumnWarps * 32) mx_quantize_columns_kernel(const T* __restrict__ x, uint32_t rows, uint32_t cols, size_t pitch, uint32_t blocks,
+                                                                                 uint32_t groups, uint32_t across, uint4* __restrict__ codes, unsigned char* __restrict__ scales)
+{
+    pdl_enter();
+    __shared__ uint4 sh_codes[kColumnWidth][kColumnPad];
+    __shared__ __align__(8) unsigned char sh_scales[kColumnWidth][kColumnWarps];
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    const uint32_t band = blockIdx.x / across, c0 = (blockIdx.x - band * across) * kColumnWidth;
+    const uint32_t c = c0 + lane * 2, b = band * kColumnWarps + warp, r0 = b * kMxBlock;
+    MxTwo<T> v[kMxBlock];
+    if (VEC && c0 + kColumnWidth <= cols && r0 + kMxBlock <= rows) {
+        const T* p = x + (size_t)r0 * pitch + c;
+#pragma unroll
+        for (int i = 0; i < kMxBlock; ++i, p += pitch) v[i] = *reinterpret_cast<const MxTwo<T>*>(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kMxBlock; ++i) {
+            const T* p = x + (size_t)(r0 + i) * pitch + c;
+            T e[2] = {mx_round<T>(0.0f), mx_round<T>(0.0f)};
+            if (r0 + i < rows) {
+                if (c < cols) e[0] = p[0];
+                if (c + 1 < cols) e[1] = p[1];
+            }
+            v[i] = *reinterpret_cast<const MxTwo<T>*>(e);
+        }
+    }
+    MxTop<T> top;
+#pragma unroll
+    for (int i = 0; i < kMxBlock; ++i) mx_top(top, v[i]);
+    const uint32_t s0 = mx_exponent(mx_first(top)), s1 = mx_exponent(mx_second(top));
+    const float i0 = mx_inverse(s0), i1 = mx_inverse(s1);
+    const uint32_t both = mx_pair(i0, i1);
+    uint32_t w0[4], w1[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        float f0[8], f1[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mx_scaled(v[8 * q + i], i0, i1, both, f0[i], f1[i]);
+        w0[q] = s0 == 255u ? 0u : mx_encode8(f0);
+        w1[q] = s1 == 255u ? 0u : mx_encode8(f1);
+    }
+    sh_codes[lane * 2][warp] = make_uint4(w0[0], w0[1], w0[2], w0[3]);
+    sh_codes[lane * 2 + 1][warp] = make_uint4(w1[0], w1[1], w1[2], w1[3]);
+    sh_scales[lane * 2][warp] = (unsigned char)s0;
+    sh_scales[lane * 2 + 1][warp] = (unsigned char)s1;
+    __syncthreads();
+    const uint32_t b0 = band * kColumnWarps;
+#pragma unroll
+    for (int i = 0; i < kColumnWidth / 32; ++i) {
+        const uint32_t column = (threadIdx.x >> 3) + 32 * i, piece = threadIdx.x & 7u;
+        if (c0 + column < cols && b0 + piece < blocks) codes[(size_t)(c0 + column) * blocks + b0 + piece] = sh_codes[column][piece];
+    }
+    if (threadIdx.x < 2 * kColumnWidth) {
+        const uint32_t column = threadIdx.x >> 1, half = threadIdx.x & 1u, g = band * 2 + half;
+        if (g < groups) *reinterpret_cast<uint32_t*>(scales + mx_scale_at(c0 + column, g, groups)) = *reinterpret_cast<const uint32_t*>(&sh_scales[column][4 * half]);
+    }
+}
+
+// Back: lanes as in mx_quantize_rows_kernel.  Where rows do not begin on 16-byte boundaries a lane takes every sixteenth element of a group instead of
+// eight neighbours, so that a store is still one run.
+template <class T, bool VEC, int STRIP>
 __global__ void __launch_bounds__(kMxThreads) mx_dequantize_kernel(const uint32_t* __restrict__ codes, const unsigned char* __restrict__ scales, uint32_t rows,
-                                                                    uint32_t cols, uint32_t blocks, uint32_t groups, uint32_t total, uint32_t step_row,
-                                                                    uint32_t step_group, T* __restrict__ y, size_t pitch)
+                                                                    uint32_t cols, uint32_t blocks, uint32_t groups, uint32_t strips, uint32_t total, uint32_t step_row,
+                                                                    uint32_t step_strip, T* __restrict__ y, size_t pitch)
 {
     pdl_enter();
     const uint32_t sub = threadIdx.x & 15u;
     uint32_t u = blockIdx.x * (kMxThreads / 16) + (threadIdx.x >> 4);
-    uint32_t r = u / groups, g = u - r * groups;
+    uint32_t r = u / strips, strip = u - r * strips;
     const uint32_t stride = gridDim.x * (kMxThreads / 16);
     for (; u < total; u += stride) {
-        const uint32_t at = g * kMxGroup + sub * 8;
-        if (at < cols) {
-            const uint32_t w = __ldcs(codes + ((size_t)r * blocks + (at >> 5)) * 4 + (sub & 3u));
-            const uint32_t s = scales[mx_scale_at(r, g, groups) + (sub >> 2)];
-            float v[8];
-            mx_decode8(w, mx_scale(s), v);
-            T* out = y + (size_t)r * pitch + at;
-            constexpr int kPer = 16 / sizeof(T);
-            if (VEC && at + 8 <= cols) {
+        const uint32_t g0 = strip * STRIP;
+        const unsigned char* const scale = scales + mx_scale_at(r, g0, groups);
+        T* const row = y + (size_t)r * pitch;
+        if (VEC) {
+            const uint32_t at = g0 * kMxGroup + sub * 8;
+            const uint32_t* const in = codes + ((size_t)r * blocks + (at >> 5)) * 4 + (sub & 3u);
+            uint32_t w[STRIP], s[STRIP];
 #pragma unroll
-                for (int i = 0; i < 8 / kPer; ++i) {
-                    MxPack<T> p;
-#pragma unroll
-                    for (int j = 0; j < kPer; ++j) p.v[j] = mx_round<T>(v[kPer * i + j]);
-                    reinterpret_cast<uint4*>(out)[i] = *reinterpret_cast<const uint4*>(&p);
+            for (int j = 0; j < STRIP; ++j)
+                if (at + j * kMxGroup < cols) {
+                    w[j] = __ldcs(in + 16 * j);
+                    s[j] = scale[j * kMxTileBytes + (sub >> 2)];
                 }
-            } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (at + i < cols) out[i] = mx_round<T>(v[i]);
+            for (int j = 0; j < STRIP; ++j) {
+                const uint32_t here = at + j * kMxGroup;
+                if (here >= cols) break;
+                float v[8];
+                mx_decode8(w[j], mx_scale(s[j]), v);
+                constexpr int kPer = 16 / sizeof(T);
+                if (here + 8 <= cols) {
+#pragma unroll
+                    for (int i = 0; i < 8 / kPer; ++i) {
+                        MxPack<T> p;
+#pragma unroll
+                        for (int q = 0; q < kPer; ++q) p.v[q] = mx_round<T>(v[kPer * i + q]);
+                        reinterpret_cast<uint4*>(row + here)[i] = *reinterpret_cast<const uint4*>(&p);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (here + i < cols) row[here + i] = mx_round<T>(v[i]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < STRIP; ++j) {
+                const uint32_t at = (g0 + j) * kMxGroup;
+                if (at >= cols) break;
+                const unsigned char* const in = reinterpret_cast<const unsigned char*>(codes) + ((size_t)r * blocks + (at >> 5)) * 16;
+                const uint32_t four = *reinterpret_cast<const uint32_t*>(scale + j * kMxTileBytes);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t e = 16 * i + sub;
+                    if (at + e < cols) row[at + e] = mx_round<T>(mx_decode1(in[e >> 1] >> (4 * (e & 1u)) & 15u) * mx_scale(four >> (8 * (i >> 1)) & 255u));
+                }
             }
         }
         r += step_row;
-        g += step_group;
-        if (g >= groups) { g -= groups; ++r; }
+        strip += step_strip;
+        if (strip >= strips) { strip -= strips; ++r; }
     }
 }
 
 struct Rounds {
+    uint32_t strips, total;
     unsigned ctas;
-    uint32_t step_row, step_group;
+    uint32_t step_row, step_strip;
 };
-// As many CTAs as there is work for, at most `most`, and how far (row, group) moves from round to round.
-Rounds rounds_of(size_t total, uint32_t groups, size_t most)
+// Strips of a row, as many CTAs as there is work for (at most 2^16), and how far (row, strip) moves from round to round.
+Rounds rounds_of(size_t rows, size_t groups, int strip)
 {
-    const size_t per = kMxThreads / 16;
-    const unsigned ctas = (unsigned)std::min((total + per - 1) / per, most);
+    const size_t per = kMxThreads / 16, strips = (groups + strip - 1) / strip, total = rows * strips;
+    const unsigned ctas = (unsigned)std::min((total + per - 1) / per, (size_t)1 << 16);
     const uint32_t stride = ctas * (uint32_t)per;
-    return {ctas, stride / groups, stride % groups};
+    return {(uint32_t)strips, (uint32_t)total, ctas, stride / (uint32_t)strips, stride % (uint32_t)strips};
+}
+// Strips of four groups where a row has that many and there are enough of them for all SMs; else of one.
+constexpr size_t kStripWork = 1 << 15;
+bool strips_pay(size_t rows, size_t groups) { return groups >= 4 && rows * groups >= kStripWork; }
+
+template <class T, bool VEC>
+cudaError_t launch_rows(const T* x, size_t rows, size_t cols, size_t pitch, void* codes, void* scales, cudaStream_t st)
+{
+    const size_t blocks = mx_blocks(cols), groups = mx_groups(cols), padded = mx_bands(rows) * kMxBand;
+    const bool four = strips_pay(padded, groups);
+    const Rounds k = rounds_of(padded, groups, four ? 4 : 1);
+    return launch_k(four ? mx_quantize_rows_kernel<T, VEC, 4> : mx_quantize_rows_kernel<T, VEC, 1>, dim3(k.ctas), dim3(kMxThreads), 0, st, x, (uint32_t)rows, (uint32_t)cols,
+                    pitch, (uint32_t)blocks, (uint32_t)groups, k.strips, k.total, k.step_row, k.step_strip, (uint32_t*)codes, (unsigned char*)scales);
 }
 
 template <class T>
@@ -194,33 +296,35 @@ int quantize(const T* x, size_t rows, size_t cols, size_t pitch, bool transpose,
     const uintptr_t at = (uintptr_t)x;
     cudaError_t e;
     if (transpose) {
-        const size_t blocks = mx_blocks(rows), groups = mx_groups(rows), across = mx_bands(cols) * 2;
-        if (groups * across > kMxMaxGroups) return ZCCL_E_ARG;
+        const size_t blocks = mx_blocks(rows), groups = mx_groups(rows), across = mx_bands(cols) * (kMxBand / kColumnWidth), down = (blocks + kColumnWarps - 1) / kColumnWarps;
+        if (down * across > kMxMaxGroups) return ZCCL_E_ARG;
         const bool vec = at % (2 * sizeof(T)) == 0 && pitch % 2 == 0;
-        e = launch_k(vec ? mx_quantize_columns_kernel<T, true> : mx_quantize_columns_kernel<T, false>, dim3((unsigned)(groups * across)), dim3(128), 0, st,
+        e = launch_k(vec ? mx_quantize_columns_kernel<T, true> : mx_quantize_columns_kernel<T, false>, dim3((unsigned)(down * across)), dim3(kColumnWarps * 32), 0, st,
                      x, (uint32_t)rows, (uint32_t)cols, pitch, (uint32_t)blocks, (uint32_t)groups, (uint32_t)across, (uint4*)codes, (unsigned char*)scales);
     } else {
-        const size_t blocks = mx_blocks(cols), groups = mx_groups(cols), total = mx_bands(rows) * kMxBand * groups;
-        if (total > kMxMaxGroups) return ZCCL_E_ARG;
-        const bool vec = at % 16 == 0 && pitch * sizeof(T) % 16 == 0;
-        const Rounds k = rounds_of(total, (uint32_t)groups, 1u << 16);
-        e = launch_k(vec ? mx_quantize_rows_kernel<T, true> : mx_quantize_rows_kernel<T, false>, dim3(k.ctas), dim3(kMxThreads), 0, st, x, (uint32_t)rows,
-                     (uint32_t)cols, pitch, (uint32_t)blocks, (uint32_t)groups, (uint32_t)total, k.step_row, k.step_group, (uint32_t*)codes, (unsigned char*)scales);
+        if (mx_bands(rows) * kMxBand * mx_groups(cols) > kMxMaxGroups) return ZCCL_E_ARG;
+        e = at % 16 == 0 && pitch * sizeof(T) % 16 == 0 ? launch_rows<T, true>(x, rows, cols, pitch, codes, scales, st) : launch_rows<T, false>(x, rows, cols, pitch, codes, scales, st);
     }
     if (e == cudaSuccess) count_launches(1);
     return e == cudaSuccess ? ZCCL_OK : ZCCL_E_CUDA;
 }
 
+template <class T, bool VEC>
+cudaError_t launch_back(const void* codes, const void* scales, size_t rows, size_t cols, T* y, size_t pitch, cudaStream_t st)
+{
+    const size_t blocks = mx_blocks(cols), groups = mx_groups(cols);
+    const bool four = strips_pay(rows, groups);
+    const Rounds k = rounds_of(rows, groups, four ? 4 : 1);
+    return launch_k(four ? mx_dequantize_kernel<T, VEC, 4> : mx_dequantize_kernel<T, VEC, 1>, dim3(k.ctas), dim3(kMxThreads), 0, st, (const uint32_t*)codes,
+                    (const unsigned char*)scales, (uint32_t)rows, (uint32_t)cols, (uint32_t)blocks, (uint32_t)groups, k.strips, k.total, k.step_row, k.step_strip, y, pitch);
+}
+
 template <class T>
 int dequantize(const void* codes, const void* scales, size_t rows, size_t cols, T* y, size_t pitch, cudaStream_t st)
 {
-    const size_t blocks = mx_blocks(cols), groups = mx_groups(cols), total = rows * groups;
-    if (total > kMxMaxGroups) return ZCCL_E_ARG;
+    if (rows * mx_groups(cols) > kMxMaxGroups) return ZCCL_E_ARG;
     const bool vec = (uintptr_t)y % 16 == 0 && pitch * sizeof(T) % 16 == 0;
-    const Rounds k = rounds_of(total, (uint32_t)groups, 1u << 16);
-    const cudaError_t e = launch_k(vec ? mx_dequantize_kernel<T, true> : mx_dequantize_kernel<T, false>, dim3(k.ctas), dim3(kMxThreads), 0, st,
-                                   (const uint32_t*)codes, (const unsigned char*)scales, (uint32_t)rows, (uint32_t)cols, (uint32_t)blocks, (uint32_t)groups,
-                                   (uint32_t)total, k.step_row, k.step_group, y, pitch);
+    const cudaError_t e = vec ? launch_back<T, true>(codes, scales, rows, cols, y, pitch, st) : launch_back<T, false>(codes, scales, rows, cols, y, pitch, st);
     if (e == cudaSuccess) count_launches(1);
     return e == cudaSuccess ? ZCCL_OK : ZCCL_E_CUDA;
 }

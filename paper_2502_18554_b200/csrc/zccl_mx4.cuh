@@ -48,8 +48,8 @@ __device__ __forceinline__ float mx_inverse(uint32_t s) { return __uint_as_float
 // 2^e; e = -127 is a subnormal number
 __device__ __forceinline__ float mx_scale(uint32_t s) { return __uint_as_float(s == 0u ? 0x00400000u : s == 255u ? 0x7FC00000u : s << 23); }
 
-// Eight values of a block times 2^-e as eight codes (the conversion rounds to nearest, ties to even, and ends at 6).
-__device__ __forceinline__ uint32_t mx_encode8(const float (&v)[8], float inverse)
+// Eight values of a block, already times 2^-e, as eight codes (the conversion rounds to nearest, ties to even, and ends at 6).
+__device__ __forceinline__ uint32_t mx_encode8(const float (&v)[8])
 {
     uint32_t w;
     asm("{\n\t.reg .b8 a, b, c, d;\n\t"
@@ -59,9 +59,15 @@ __device__ __forceinline__ uint32_t mx_encode8(const float (&v)[8], float invers
         "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
         "mov.b32 %0, {a, b, c, d};\n\t}"
         : "=r"(w)
-        : "f"(v[0] * inverse), "f"(v[1] * inverse), "f"(v[2] * inverse), "f"(v[3] * inverse),
-          "f"(v[4] * inverse), "f"(v[5] * inverse), "f"(v[6] * inverse), "f"(v[7] * inverse));
+        : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
     return w;
+}
+// One code (four bits): magnitudes 0 ... 3 are halves of their index, 4 ... 7 have two mantissas to a binade.
+__device__ __forceinline__ float mx_decode1(uint32_t code)
+{
+    const uint32_t m = code & 7u;
+    // E2M1 moved to binary32's exponent and mantissa is the value times 2^-126, its subnormal number one of binary32's
+    return __uint_as_float(m << 22 | (code & 8u) << 28) * 0x1p126f;
 }
 __device__ __forceinline__ void mx_decode8(uint32_t w, float scale, float (&v)[8])
 {

@@ -29,20 +29,8 @@ struct Product {
     uint32_t depth_blocks;                    // blocks of 32 along the contraction
     uint32_t row_tiles, col_tiles;
     int type;
+    int wide;                                 // every row of y begins on a 16-byte boundary
     int across;                               // 1: y is stored the other way round, its rows along the kernel's columns
-};
-
-template <int BN>
-struct ProductShape {
-    static constexpr int kBands = BN > 128 ? 2 : 1;           // tiles of scales that a tile's columns lie in
-    static constexpr int kRowCodes = kRows * kRowBytes, kColCodes = BN * kRowBytes;
-    static constexpr int kColAt = kRowCodes, kRowScaleAt = kColAt + kColCodes, kColScaleAt = kRowScaleAt + 2 * kMxTileBytes;
-    static constexpr int kStage = kColScaleAt + 2 * kMxTileBytes * kBands;
-    static constexpr int kScaleColumns = 8 + 8 * kBands;      // of tensor memory, for one stage
-};
-
-struct Control {
-    unsigned long long *full, *empty, *done, *free;
 };
 
 __device__ __forceinline__ bool wait_for(unsigned long long* bar, uint32_t parity)
@@ -52,221 +40,377 @@ __device__ __forceinline__ bool wait_for(unsigned long long* bar, uint32_t parit
     atomicOr(&g_product_status, kStuck);
     return false;
 }
+__device__ __forceinline__ bool wait_for_cluster(unsigned long long* bar, uint32_t parity)
+{
+    for (uint32_t i = 0; i < kWaitLimit; ++i)
+        if (mbar_try_wait_cluster(bar, parity)) return true;
+    atomicOr(&g_product_status, kStuck);
+    return false;
+}
+__device__ __forceinline__ unsigned char* on_1024(unsigned char* raw) { return raw + (1024 - (smem_u32(raw) & 1023u)) % 1024; }
 
 // How much of the contraction is left from depth tile k on, in groups of 128 (0, 1 or 2) and instructions (up to 4).
 __device__ __forceinline__ uint32_t groups_at(uint32_t k, uint32_t blocks) { return min(2u, (blocks - k * 8 + 3) / 4); }
 __device__ __forceinline__ uint32_t steps_at(uint32_t k, uint32_t blocks) { return min(4u, (blocks - k * 8 + 1) / 2); }
 
-template <class T>
-__device__ __forceinline__ void store_row(T* y, uint32_t count, const uint32_t (&v)[32])
+__device__ __forceinline__ void store_one(const Product& k, size_t to, float v)
 {
-    if (count == 32 && ((uintptr_t)y & 15u) == 0) {
-        constexpr int kPer = 16 / sizeof(T);
-#pragma unroll
-        for (int i = 0; i < 32 / kPer; ++i) {
-            MxPack<T> p;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) p.v[j] = mx_round<T>(__uint_as_float(v[kPer * i + j]));
-            reinterpret_cast<uint4*>(y)[i] = *reinterpret_cast<const uint4*>(&p);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (i < (int)count) y[i] = mx_round<T>(__uint_as_float(v[i]));
-    }
-}
-// Up to 32 sums of a lane, columns c ... of row r.
-template <class T>
-__device__ __forceinline__ void store(const Product& k, uint32_t r, uint32_t c, uint32_t width, const uint32_t (&v)[32])
-{
-    if (r >= k.rows || c >= k.cols) return;
-    const uint32_t count = min(width, k.cols - c);
-    T* y = (T*)k.y;
-    if (k.across) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (i < (int)count) y[(size_t)(c + i) * k.pitch + r] = mx_round<T>(__uint_as_float(v[i]));
-    } else store_row(y + (size_t)r * k.pitch + c, count, v);
-}
-__device__ __forceinline__ void store_any(const Product& k, uint32_t r, uint32_t c, uint32_t width, const uint32_t (&v)[32])
-{
-    if (k.type == ZCCL_BF16) store<__nv_bfloat16>(k, r, c, width, v);
-    else if (k.type == ZCCL_F16) store<__half>(k, r, c, width, v);
-    else store<float>(k, r, c, width, v);
+    if (k.type == ZCCL_BF16) ((__nv_bfloat16*)k.y)[to] = mx_round<__nv_bfloat16>(v);
+    else if (k.type == ZCCL_F16) ((__half*)k.y)[to] = mx_round<__half>(v);
+    else ((float*)k.y)[to] = v;
 }
 
-// Tile t of the output: eight tiles of rows share a walk along the columns, so what is in flight reads few rows and columns.
-__device__ __forceinline__ void tile_of(const Product& k, uint32_t t, uint32_t& row_tile, uint32_t& col_tile)
+// Tile t of the output: `high` tiles of rows share a walk along the columns, so what is in flight reads few rows and columns.
+__device__ __forceinline__ void tile_of(const Product& k, uint32_t t, uint32_t band_tiles, uint32_t& row_tile, uint32_t& col_tile)
 {
-    constexpr uint32_t kBand = 8;
-    const uint32_t per = kBand * k.col_tiles, band = t / per, in = t - band * per;
-    const uint32_t high = min(kBand, k.row_tiles - band * kBand);
+    const uint32_t per = band_tiles * k.col_tiles, band = t / per, in = t - band * per;
+    const uint32_t high = min(band_tiles, k.row_tiles - band * band_tiles);
     col_tile = in / high;
-    row_tile = band * kBand + (in - col_tile * high);
+    row_tile = band * band_tiles + (in - col_tile * high);
 }
 
-// One CTA (SPLIT: one cluster) per tile of 128 x BN at a time.  SPLIT: the CTAs of a cluster take neighbouring pieces of the contraction
-// of one tile; their sums are added in the order of the pieces out of each other's shared memory, each CTA some of the columns.
-template <int BN, int STAGES, bool SPLIT>
-__global__ void __launch_bounds__(kProductThreads, 1) mx4_product_kernel(const __grid_constant__ CUtensorMap r_map, const __grid_constant__ CUtensorMap c_map, const __grid_constant__ Product k)
+// ---------------------------------------------------------------- few rows, or few tiles
+
+// A tile of 128 x BN to a cluster, whose CTAs take neighbouring pieces of the contraction.  Their sums are added in the order of the
+// pieces out of each other's shared memory, each CTA some of the columns (or rows), so there is no workspace and no order that changes.
+// Bound by latency, or for weights that do not stay in L2 by memory.  The few rows go along the instruction's columns (16 at least), the many along
+// its 128 lanes: a stage is then little else than the weights.  More than one CTA to an SM: none allocates more tensor memory than its
+// share by shared memory (kSplitColumns), or clusters could wait for each other's.
+template <int BN>
+struct SplitShape {
+    static constexpr int kStages = BN == 128 ? 3 : 4;
+    static constexpr int kColAt = kRows * kRowBytes, kRowScaleAt = kColAt + BN * kRowBytes, kColScaleAt = kRowScaleAt + 2 * kMxTileBytes;
+    static constexpr int kStage = kColScaleAt + 2 * kMxTileBytes;
+    static constexpr int kScaleColumns = 16;                                     // of tensor memory, for one stage
+    static constexpr int kSumColumns = BN < 32 ? 32 : BN;
+    static constexpr int kColumns = BN <= 32 ? 64 : BN == 64 ? 128 : 256;
+    static constexpr int kSumPitch = kRows + 1;                                  // floats: sums are read along rows and along columns
+    static constexpr size_t kBytes = (size_t)kStage * kStages + 1024;
+    static_assert(kSumColumns + 2 * kScaleColumns <= kColumns, "tensor memory");
+    static_assert(BN * kSumPitch * 4 <= kStage * kStages, "sums take the stages' place");
+    static_assert((228 * 1024 / kBytes) * kColumns <= 512, "clusters must not wait for each other's tensor memory");
+};
+
+template <int BN>
+__global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __grid_constant__ CUtensorMap r_map, const __grid_constant__ CUtensorMap c_map, const __grid_constant__ Product k)
 {
-    using S = ProductShape<BN>;
-    constexpr int kSums = SPLIT ? 1 : 2;
-    constexpr uint32_t kSumColumns = BN < 32 ? 32 : BN;
-    constexpr uint32_t kNeed = kSums * kSumColumns + 2 * S::kScaleColumns;
-    constexpr uint32_t kColumns = kNeed <= 64 ? 64 : kNeed <= 128 ? 128 : kNeed <= 256 ? 256 : 512;
-    static_assert(kNeed <= 512, "tensor memory");
+    using S = SplitShape<BN>;
+    constexpr int kStages = S::kStages;
     extern __shared__ unsigned char raw[];
-    __shared__ unsigned long long full[STAGES], empty[STAGES], done[2], free_[2], drained;
+    __shared__ unsigned long long full[kStages], empty[kStages], done;
     __shared__ uint32_t tmem_at;
-    unsigned char* const tiles = raw + (1024 - (smem_u32(raw) & 1023u)) % 1024;
+    unsigned char* const tiles = on_1024(raw);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
 
     if (warp == 0 && lane == 0) {
         prefetch_map(&r_map);
         prefetch_map(&c_map);
-        for (int i = 0; i < STAGES; ++i) {
+        for (int i = 0; i < kStages; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], 1);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&done[i], 1);
-            mbar_init(&free_[i], 4);
-        }
-        mbar_init(&drained, 1);
+        mbar_init(&done, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) tmem_alloc(&tmem_at, kColumns);
+    if (warp == 1) tmem_alloc(&tmem_at, S::kColumns);
     tcgen05_fence_before();
     __syncthreads();
     tcgen05_fence_after();
     const uint32_t tmem = tmem_at;
     pdl_enter();
 
-    const uint32_t depth_tiles = (k.depth_blocks + 7) / 8, total = k.row_tiles * k.col_tiles;
-    uint32_t first_tile = blockIdx.x, stride = gridDim.x, k_begin = 0, k_end = depth_tiles, parts = 1, part = 0;
-    if (SPLIT) {
-        asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
-        part = cluster_rank();
-        first_tile = blockIdx.x / parts;
-        stride = total;                        // one tile
-        k_begin = (uint32_t)((unsigned long long)depth_tiles * part / parts);
-        k_end = (uint32_t)((unsigned long long)depth_tiles * (part + 1) / parts);
-    }
+    uint32_t parts;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
+    const uint32_t depth_tiles = (k.depth_blocks + 7) / 8, part = cluster_rank();
+    const uint32_t k_begin = (uint32_t)((unsigned long long)depth_tiles * part / parts), k_end = (uint32_t)((unsigned long long)depth_tiles * (part + 1) / parts);
+    uint32_t rt, ct;
+    tile_of(k, blockIdx.x / parts, 8, rt, ct);
+    const uint32_t c0 = ct * BN;
 
     if (warp == 0) {
         if (lane == 0) {
-            const uint32_t groups = (k.depth_blocks + 3) / 4, col_bands = (k.cols + kMxBand - 1) / kMxBand;
+            const uint32_t groups = (k.depth_blocks + 3) / 4;
             uint32_t n = 0;
-            bool ok = true;
-            for (uint32_t t = first_tile; t < total && ok; t += stride) {
-                uint32_t rt, ct;
-                tile_of(k, t, rt, ct);
-                const uint32_t c0 = ct * BN, band = c0 / kMxBand, bands = min((uint32_t)S::kBands, col_bands - band);
-                for (uint32_t d = k_begin; d < k_end; ++d, ++n) {
-                    const uint32_t s = n % STAGES;
-                    if (n >= STAGES && !(ok = wait_for(&empty[s], (n / STAGES - 1) & 1))) break;
-                    unsigned char* const at = tiles + s * S::kStage;
-                    const uint32_t scale_bytes = groups_at(d, k.depth_blocks) * kMxTileBytes;
-                    mbar_expect_tx(&full[s], S::kRowCodes + S::kColCodes + scale_bytes * (1 + bands));
-                    tile_load(at, &r_map, (int)(d * kRowBytes), (int)(rt * kRows), &full[s]);
-                    tile_load(at + S::kColAt, &c_map, (int)(d * kRowBytes), (int)c0, &full[s]);
-                    bytes_load(at + S::kRowScaleAt, k.r_scales + ((size_t)rt * groups + 2 * d) * kMxTileBytes, scale_bytes, &full[s]);
-                    for (uint32_t b = 0; b < bands; ++b)
-                        bytes_load(at + S::kColScaleAt + b * 2 * kMxTileBytes, k.c_scales + ((size_t)(band + b) * groups + 2 * d) * kMxTileBytes, scale_bytes, &full[s]);
-                }
+            for (uint32_t d = k_begin; d < k_end; ++d, ++n) {
+                const uint32_t s = n % kStages;
+                if (n >= kStages && !wait_for(&empty[s], (n / kStages - 1) & 1)) break;
+                unsigned char* const at = tiles + s * S::kStage;
+                const uint32_t scale_bytes = groups_at(d, k.depth_blocks) * kMxTileBytes;
+                mbar_expect_tx(&full[s], (kRows + BN) * kRowBytes + 2 * scale_bytes);
+                tile_load(at, &r_map, (int)(d * kRowBytes), (int)(rt * kRows), &full[s]);
+                tile_load(at + S::kColAt, &c_map, (int)(d * kRowBytes), (int)c0, &full[s]);
+                bytes_load(at + S::kRowScaleAt, k.r_scales + ((size_t)rt * groups + 2 * d) * kMxTileBytes, scale_bytes, &full[s]);
+                bytes_load(at + S::kColScaleAt, k.c_scales + ((size_t)(c0 / kMxBand) * groups + 2 * d) * kMxTileBytes, scale_bytes, &full[s]);
             }
             // what has been asked for lands before the memory is given up, whether it is used or not
-            for (uint32_t i = n < STAGES ? 0 : n - STAGES; i < n; ++i) wait_for(&full[i % STAGES], (i / STAGES) & 1);
+            for (uint32_t i = n < kStages ? 0 : n - kStages; i < n; ++i) wait_for(&full[i % kStages], (i / kStages) & 1);
         }
     } else if (warp == 1) {
         if (elect_one()) {
+            uint32_t n = 0;
+            for (uint32_t d = k_begin; d < k_end; ++d, ++n) {
+                const uint32_t s = n % kStages;
+                if (!wait_for(&full[s], (n / kStages) & 1)) break;
+                tcgen05_fence_after();
+                const uint32_t at = smem_u32(tiles) + s * S::kStage;
+                const uint32_t r_scale = tmem + S::kSumColumns + (n & 1) * S::kScaleColumns, c_scale = r_scale + 8;
+                for (uint32_t g = 0; g < groups_at(d, k.depth_blocks); ++g) {
+                    tcgen05_copy_scales(r_scale + 4 * g, scales_descriptor(at + S::kRowScaleAt + g * kMxTileBytes));
+                    tcgen05_copy_scales(c_scale + 4 * g, scales_descriptor(at + S::kColScaleAt + g * kMxTileBytes));
+                }
+                const unsigned long long r_codes = operand_descriptor(at), c_codes = operand_descriptor(at + S::kColAt);
+                const uint32_t steps = steps_at(d, k.depth_blocks), shift = BN < kMxBand ? (c0 % kMxBand) / 32 : 0;
+                for (uint32_t j = 0; j < steps; ++j)
+                    tcgen05_mma_mx4(tmem, r_codes + 2 * j, c_codes + 2 * j, mx4_instruction(kRows, BN, (j & 1) * 2), r_scale + 4 * (j / 2), c_scale + 4 * (j / 2) + shift,
+                                    n > 0 || j > 0);
+                tcgen05_commit(&empty[s]);
+            }
+            tcgen05_commit(&done);
+            wait_for(&done, 0);
+        }
+    } else if (wait_for(&done, 0)) {
+        tcgen05_fence_after();
+        const uint32_t quarter = warp & 3u, row = quarter * 32 + lane;
+        constexpr int kWide = BN < 32 ? BN : 32;
+#pragma unroll 1
+        for (int c = 0; c < BN; c += kWide) {
+            uint32_t v[32];
+            if (kWide == 32) tcgen05_load32(tmem + (quarter * 32 << 16) + c, v);
+            else tcgen05_load16(tmem + (quarter * 32 << 16) + c, v);
+            tcgen05_wait_loads();
+#pragma unroll
+            for (int j = 0; j < kWide; ++j) reinterpret_cast<float*>(tiles)[(c + j) * S::kSumPitch + row] = __uint_as_float(v[j]);
+        }
+        tcgen05_fence_before();
+    }
+    __syncwarp();
+    cluster_sync();
+    if (warp >= 2) {
+        const uint32_t sums = smem_u32(tiles), r0 = rt * kRows;
+        if (k.across) {
+            const uint32_t row = threadIdx.x - 64;
+            for (uint32_t c = part; c < (uint32_t)BN && c0 + c < k.cols; c += parts) {
+                float sum = 0.0f;
+                for (uint32_t p = 0; p < parts; ++p) sum += peer_load(sums + (c * S::kSumPitch + row) * 4, p);
+                if (r0 + row < k.rows) store_one(k, (size_t)(c0 + c) * k.pitch + r0 + row, sum);
+            }
+        } else {
+            for (uint32_t row = part * 4 + warp - 2; row < kRows && r0 + row < k.rows; row += 4 * parts)
+#pragma unroll 4
+                for (uint32_t c = lane; c < (uint32_t)BN; c += 32) {
+                    float sum = 0.0f;
+                    for (uint32_t p = 0; p < parts; ++p) sum += peer_load(sums + (c * S::kSumPitch + row) * 4, p);
+                    if (c0 + c < k.cols) store_one(k, (size_t)(r0 + row) * k.pitch + c0 + c, sum);
+                }
+        }
+    }
+    __syncwarp();
+    cluster_sync();                        // nobody leaves while its sums are still read
+    if (warp == 1) tmem_free(tmem, S::kColumns);
+}
+
+// ---------------------------------------------------------------- many tiles
+
+// A pair of CTAs (the two of a cluster) works on a tile of 256 x BN: the first issues instructions that use both tensor cores, each CTA brings and
+// keeps its 128 rows of one operand and half of the other, so an SM reads 128 + BN / 2 rows for 128 x BN sums.  What bounds it is the
+// way from L2 to shared memory: with tiles of 128 x 192 to a single CTA the large product took 157 us (4096 x 8192 x 8192), 12 TB/s.
+// Sums of 256 columns do not fit tensor memory twice next to the scales, so the second set begins 24 columns inside the first; whoever
+// reads sums out begins with the columns that both have, and says when these are free.
+template <int BN>
+struct PairShape {
+    static constexpr int kStages = BN == 256 ? 5 : 7;
+    static constexpr int kBands = BN / kMxBand;                                  // tiles of scales that a tile's columns lie in
+    static constexpr int kColAt = kRows * kRowBytes, kRowScaleAt = kColAt + BN / 2 * kRowBytes, kColScaleAt = kRowScaleAt + 2 * kMxTileBytes;
+    static constexpr int kStage = kColScaleAt + 2 * kMxTileBytes * kBands;
+    static constexpr bool kOverlap = BN == 256;
+    static constexpr int kScaleColumns = 8 + 8 * kBands;                         // for one stage; two sets of them
+    static constexpr int kShared = kOverlap ? 2 * kScaleColumns : 0;             // columns that both sets of sums have
+    static constexpr int kSecond = BN - kShared;                                 // where the second set of sums begins
+    static constexpr int kScaleAt = kSecond + BN;
+    static constexpr int kColumns = 512;
+    static constexpr int kOutPitch = 128 + 16;                                   // bytes of a row on its way out
+    static constexpr size_t kBytes = (size_t)kStage * kStages + 4 * 32 * kOutPitch + 1024;
+    static_assert(kScaleAt + 2 * kScaleColumns <= kColumns, "tensor memory");
+    static_assert(kBytes <= 227 * 1024 && kBytes > 114 * 1024, "one CTA to an SM");
+};
+
+// 128 bytes of each of the warp's 32 rows, from registers through shared memory: rows leave as whole lines, or where they do not begin on 16 bytes as runs
+// of neighbouring elements.  T is the type of the output, `v` has 128 / sizeof(T) columns of the lane's row from c on.
+template <class T>
+__device__ __forceinline__ void store_rows(const Product& k, unsigned char* out, uint32_t r, uint32_t c, const float (&v)[128 / sizeof(T)])
+{
+    constexpr int kPitch = 128 + 16, kPer = 16 / sizeof(T), kWidth = 128 / sizeof(T);
+    const uint32_t lane = threadIdx.x & 31u;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        MxPack<T> p;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) p.v[j] = mx_round<T>(v[kPer * i + j]);
+        *reinterpret_cast<uint4*>(out + lane * kPitch + 16 * i) = *reinterpret_cast<const uint4*>(&p);
+    }
+    __syncwarp();
+    T* const y = (T*)k.y + (size_t)r * k.pitch + c;
+    const uint32_t high = r < k.rows ? min(32u, k.rows - r) : 0u;
+    if (k.wide && c + kWidth <= k.cols) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t row = 4 * i + (lane >> 3), piece = lane & 7u;
+            if (row < high) reinterpret_cast<uint4*>(y + (size_t)row * k.pitch)[piece] = *reinterpret_cast<const uint4*>(out + row * kPitch + 16 * piece);
+        }
+    } else {
+        for (uint32_t row = 0; row < high; ++row)
+#pragma unroll
+            for (int i = 0; i < kWidth / 32; ++i) {
+                const uint32_t at = lane + 32 * i;
+                if (c + at < k.cols) y[(size_t)row * k.pitch + at] = *reinterpret_cast<const T*>(out + row * kPitch + at * sizeof(T));
+            }
+    }
+}
+
+// The sums of one tile out of tensor memory; `drained` is called once, when the columns that the next tile's sums begin in are free.
+template <class T, int BN, class F>
+__device__ __forceinline__ void store_tile(const Product& k, unsigned char* out, uint32_t sums, uint32_t r, uint32_t c0, bool from_end, F&& drained)
+{
+    constexpr int kWidth = 128 / sizeof(T), kPieces = BN / kWidth;
+#pragma unroll 1
+    for (int i = 0; i < kPieces; ++i) {
+        const uint32_t c = (uint32_t)(from_end ? kPieces - 1 - i : i) * kWidth;
+        float v[kWidth];
+#pragma unroll
+        for (int h = 0; h < kWidth / 32; ++h) tcgen05_load32(sums + c + 32 * h, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * h]));
+        tcgen05_wait_loads();
+        if (i == (PairShape<BN>::kOverlap ? (PairShape<BN>::kShared - 1) / kWidth : kPieces - 1)) {
+            tcgen05_fence_before();
+            drained();
+        }
+        store_rows<T>(k, out, r, c0 + c, v);
+    }
+}
+
+template <int BN>
+__global__ void __launch_bounds__(kProductThreads, 1) mx4_pair_kernel(const __grid_constant__ CUtensorMap r_map, const __grid_constant__ CUtensorMap c_map, const __grid_constant__ CUtensorMap r_scale_map,
+                                                                      const __grid_constant__ CUtensorMap c_scale_map, const __grid_constant__ Product k)
+{
+    using S = PairShape<BN>;
+    constexpr int kStages = S::kStages;
+    extern __shared__ unsigned char raw[];
+    __shared__ unsigned long long full[kStages], empty[kStages], done[2], free_[2], drained;
+    __shared__ uint32_t tmem_at;
+    unsigned char* const tiles = on_1024(raw);
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, rank = cluster_rank();
+
+    if (warp == 0 && lane == 0) {
+        prefetch_map(&r_map);
+        prefetch_map(&c_map);
+        prefetch_map(&r_scale_map);
+        prefetch_map(&c_scale_map);
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&done[i], 1);
+            mbar_init(&free_[i], 8);
+        }
+        mbar_init(&drained, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc_pair(&tmem_at, S::kColumns);
+    tcgen05_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tcgen05_fence_after();
+    const uint32_t tmem = tmem_at;
+    pdl_enter();
+
+    const uint32_t depth_tiles = (k.depth_blocks + 7) / 8, total = k.row_tiles * k.col_tiles, first = blockIdx.x / 2, stride = gridDim.x / 2;
+    constexpr uint32_t kBand = 8;                   // tiles of rows that share a walk
+
+    if (warp == 0) {
+        if (lane == 0) {
+            // what lands in either CTA counts at the first one's barrier
+            constexpr uint32_t kBoth = 2 * ((kRows + BN / 2) * kRowBytes + 2 * kMxTileBytes * (1 + S::kBands));
+            uint32_t n = 0;
+            bool ok = true;
+            for (uint32_t t = first; t < total && ok; t += stride) {
+                uint32_t rt, ct;
+                tile_of(k, t, kBand, rt, ct);
+                const int row_band = (int)(rt * 2 + rank), c0 = (int)(ct * BN + rank * (BN / 2));
+                for (uint32_t d = 0; d < depth_tiles; ++d, ++n) {
+                    const uint32_t s = n % kStages;
+                    if (n >= kStages && !(ok = wait_for_cluster(&empty[s], (n / kStages - 1) & 1))) break;
+                    unsigned char* const at = tiles + s * S::kStage;
+                    const uint32_t bar = address_at(&full[s], 0);
+                    if (rank == 0) mbar_expect_tx(&full[s], kBoth);
+                    tile_load_pair(at, &r_map, (int)(d * kRowBytes), row_band * kRows, bar);
+                    tile_load_pair(at + S::kColAt, &c_map, (int)(d * kRowBytes), c0, bar);
+                    scales_load_pair(at + S::kRowScaleAt, &r_scale_map, (int)(2 * d), row_band, bar);
+                    scales_load_pair(at + S::kColScaleAt, &c_scale_map, (int)(2 * d), (int)(ct * S::kBands), bar);
+                }
+            }
+            // what has been asked for lands before the memory is given up, whether it is used or not: the first CTA sees all of it
+            if (rank == 0)
+                for (uint32_t i = n < kStages ? 0 : n - kStages; i < n; ++i) wait_for(&full[i % kStages], (i / kStages) & 1);
+        }
+    } else if (warp == 1) {
+        if (rank == 0 && elect_one()) {
             uint32_t n = 0, i = 0;
             bool ok = true;
-            for (uint32_t t = first_tile; t < total && ok; t += stride, ++i) {
-                uint32_t rt, ct;
-                tile_of(k, t, rt, ct);
-                const uint32_t sums = tmem + (SPLIT ? 0 : (i & 1) * kSumColumns);
-                const uint32_t shift = (ct * BN % kMxBand) / 32;      // where the tile's columns begin in their first tile of scales
-                if (i >= kSums) {
-                    if (!(ok = wait_for(&free_[i & 1], (i / 2 - 1) & 1))) break;
+            for (uint32_t t = first; t < total && ok; t += stride, ++i) {
+                const uint32_t sums = tmem + (i & 1) * S::kSecond;
+                if (S::kOverlap ? i >= 1 : i >= 2) {
+                    if (!(ok = S::kOverlap ? wait_for_cluster(&free_[0], (i - 1) & 1) : wait_for_cluster(&free_[i & 1], (i / 2 - 1) & 1))) break;
                     tcgen05_fence_after();
                 }
-                for (uint32_t d = k_begin; d < k_end; ++d, ++n) {
-                    const uint32_t s = n % STAGES;
-                    if (!(ok = wait_for(&full[s], (n / STAGES) & 1))) break;
+                for (uint32_t d = 0; d < depth_tiles; ++d, ++n) {
+                    const uint32_t s = n % kStages, parity = (n / kStages) & 1;
+                    if (!(ok = wait_for_cluster(&full[s], parity))) break;
                     tcgen05_fence_after();
                     const uint32_t at = smem_u32(tiles) + s * S::kStage;
-                    const uint32_t r_scale = tmem + kSums * kSumColumns + (n & 1) * S::kScaleColumns, c_scale = r_scale + 8;
+                    const uint32_t r_scale = tmem + S::kScaleAt + (n & 1) * S::kScaleColumns, c_scale = r_scale + 8;
                     for (uint32_t g = 0; g < groups_at(d, k.depth_blocks); ++g) {
-                        tcgen05_copy_scales(r_scale + 4 * g, scales_descriptor(at + S::kRowScaleAt + g * kMxTileBytes));
+                        tcgen05_copy_scales_pair(r_scale + 4 * g, scales_descriptor(at + S::kRowScaleAt + g * kMxTileBytes));
+#pragma unroll
                         for (int b = 0; b < S::kBands; ++b)
-                            tcgen05_copy_scales(c_scale + 4 * (g * S::kBands + b), scales_descriptor(at + S::kColScaleAt + (b * 2 + g) * kMxTileBytes));
+                            tcgen05_copy_scales_pair(c_scale + 4 * (g * S::kBands + b), scales_descriptor(at + S::kColScaleAt + (b * 2 + g) * kMxTileBytes));
                     }
                     const unsigned long long r_codes = operand_descriptor(at), c_codes = operand_descriptor(at + S::kColAt);
                     const uint32_t steps = steps_at(d, k.depth_blocks);
                     for (uint32_t j = 0; j < steps; ++j)
-                        tcgen05_mma_mx4(sums, r_codes + 2 * j, c_codes + 2 * j, mx4_instruction(kRows, BN, (j & 1) * 2), r_scale + 4 * (j / 2),
-                                        c_scale + 4 * S::kBands * (j / 2) + shift, d > k_begin || j > 0);
-                    tcgen05_commit(&empty[s]);
+                        tcgen05_mma_mx4_pair(sums, r_codes + 2 * j, c_codes + 2 * j, mx4_instruction(2 * kRows, BN, (j & 1) * 2), r_scale + 4 * (j / 2),
+                                             c_scale + 4 * S::kBands * (j / 2), d > 0 || j > 0);
+                    tcgen05_commit_pair(&empty[s]);
                 }
-                tcgen05_commit(&done[i & 1]);
+                tcgen05_commit_pair(&done[i & 1]);
             }
-            tcgen05_commit(&drained);
-            wait_for(&drained, 0);
+            tcgen05_commit_pair(&drained);
+            wait_for_cluster(&drained, 0);
         }
     } else {
-        const uint32_t quarter = warp & 3u, row = quarter * 32 + lane;
+        const uint32_t quarter = warp & 3u;
+        unsigned char* const out = tiles + S::kStage * kStages + quarter * 32 * S::kOutPitch;
         uint32_t i = 0;
-        for (uint32_t t = first_tile; t < total; t += stride, ++i) {
+        for (uint32_t t = first; t < total; t += stride, ++i) {
             uint32_t rt, ct;
-            tile_of(k, t, rt, ct);
-            const uint32_t sums = tmem + (SPLIT ? 0 : (i & 1) * kSumColumns) + (quarter * 32 << 16);
-            if (!wait_for(&done[i & 1], (i / 2) & 1)) break;
+            tile_of(k, t, kBand, rt, ct);
+            const uint32_t b = i & 1, sums = tmem + b * S::kSecond + (quarter * 32 << 16), r = (rt * 2 + rank) * kRows + quarter * 32;
+            if (!wait_for_cluster(&done[b], (i / 2) & 1)) break;
             tcgen05_fence_after();
-            constexpr int kWide = BN < 32 ? BN : 32;
-#pragma unroll 1
-            for (int c = 0; c < BN; c += kWide) {
-                uint32_t v[32];
-                if (kWide == 32) tcgen05_load32(sums + c, v);
-                else tcgen05_load16(sums + c, v);
-                tcgen05_wait_loads();
-                if (SPLIT) {
-#pragma unroll
-                    for (int j = 0; j < kWide; ++j) reinterpret_cast<float*>(tiles)[(c + j) * kRows + row] = __uint_as_float(v[j]);
-                } else store_any(k, rt * kRows + row, ct * BN + c, kWide, v);
-            }
-            tcgen05_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&free_[i & 1]);
+            const auto free_sums = [&] {
+                __syncwarp();
+                if (lane == 0) mbar_arrive_at(&free_[S::kOverlap ? 0 : b], 0);
+            };
+            if (k.type == ZCCL_BF16) store_tile<__nv_bfloat16, BN>(k, out, sums, r, ct * BN, b == 0, free_sums);
+            else if (k.type == ZCCL_F16) store_tile<__half, BN>(k, out, sums, r, ct * BN, b == 0, free_sums);
+            else store_tile<float, BN>(k, out, sums, r, ct * BN, b == 0, free_sums);
         }
     }
-    if (SPLIT) {
-        __syncwarp();
-        cluster_sync();
-        if (warp >= 2) {
-            uint32_t rt, ct;
-            tile_of(k, first_tile, rt, ct);
-            const uint32_t row = threadIdx.x - 64;
-            for (uint32_t c = part; c < (uint32_t)BN && ct * BN + c < k.cols; c += parts) {
-                float sum = 0.0f;
-                for (uint32_t p = 0; p < parts; ++p) sum += peer_load(smem_u32(tiles) + (c * kRows + row) * 4, p);
-                const uint32_t r = rt * kRows + row, cc = ct * BN + c;
-                if (r < k.rows) {
-                    const size_t to = k.across ? (size_t)cc * k.pitch + r : (size_t)r * k.pitch + cc;
-                    if (k.type == ZCCL_BF16) ((__nv_bfloat16*)k.y)[to] = mx_round<__nv_bfloat16>(sum);
-                    else if (k.type == ZCCL_F16) ((__half*)k.y)[to] = mx_round<__half>(sum);
-                    else ((float*)k.y)[to] = sum;
-                }
-            }
-        }
-        __syncwarp();
-        cluster_sync();                        // nobody leaves while its sums are still read
-    }
-    tcgen05_fence_before();
-    __syncthreads();
     __syncwarp();
-    if (warp == 1) tmem_free(tmem, kColumns);
+    tcgen05_fence_before();
+    cluster_sync();                        // neither leaves while the other still reaches its barriers or its tensor memory
+    tcgen05_fence_after();
+    if (warp == 1) tmem_free_pair(tmem, S::kColumns);
 }
 
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
@@ -276,17 +420,14 @@ std::mutex g_product_mu;
 EncodeFn g_product_encode = nullptr;
 struct ProductDevice {
     bool ready = false;
-    int sms = 0;
+    int sms = 0, pairs = 0;       // pairs of CTAs that are resident together
 };
 ProductDevice g_product_dev[kMaxDevices];
 
-template <int BN, int STAGES, bool SPLIT>
-constexpr size_t product_smem() { return (size_t)ProductShape<BN>::kStage * STAGES + 1024; }
-template <int BN, int STAGES, bool SPLIT>
-cudaError_t product_attr()
-{
-    return cudaFuncSetAttribute(mx4_product_kernel<BN, STAGES, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)product_smem<BN, STAGES, SPLIT>());
-}
+template <int BN>
+cudaError_t split_attr() { return cudaFuncSetAttribute(mx4_split_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SplitShape<BN>::kBytes); }
+template <int BN>
+cudaError_t pair_attr() { return cudaFuncSetAttribute(mx4_pair_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairShape<BN>::kBytes); }
 
 cudaError_t product_device(const ProductDevice** out)
 {
@@ -306,13 +447,25 @@ cudaError_t product_device(const ProductDevice** out)
     ProductDevice& d = g_product_dev[dev];
     if (!d.ready) {
         e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev);
-        if (e == cudaSuccess) e = product_attr<192, 5, false>();
-        if (e == cudaSuccess) e = product_attr<128, 6, false>();
-        if (e == cudaSuccess) e = product_attr<128, 3, true>();
-        if (e == cudaSuccess) e = product_attr<64, 4, true>();
-        if (e == cudaSuccess) e = product_attr<32, 4, true>();
-        if (e == cudaSuccess) e = product_attr<16, 4, true>();
+        if (e == cudaSuccess) e = split_attr<16>();
+        if (e == cudaSuccess) e = split_attr<32>();
+        if (e == cudaSuccess) e = split_attr<64>();
+        if (e == cudaSuccess) e = split_attr<128>();
+        if (e == cudaSuccess) e = pair_attr<128>();
+        if (e == cudaSuccess) e = pair_attr<256>();
         if (e != cudaSuccess) return e;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)d.sms / 2 * 2);
+        cfg.blockDim = dim3(kProductThreads);
+        cfg.dynamicSmemBytes = PairShape<256>::kBytes;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        e = cudaOccupancyMaxActiveClusters(&d.pairs, mx4_pair_kernel<256>, &cfg);
+        if (e != cudaSuccess) return e;
+        if (d.pairs < 1) return cudaErrorNotSupported;
         d.ready = true;
     }
     *out = &d;
@@ -327,24 +480,50 @@ bool operand_map(CUtensorMap* map, const void* codes, size_t rows, size_t blocks
                             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Tiles of scales as [bands][groups][512 bytes]; a box is two groups of `bands` bands.
+bool scales_map(CUtensorMap* map, const void* scales, size_t rows, size_t blocks, int bands)
+{
+    const size_t groups = (blocks + 3) / 4;
+    const cuuint64_t size[3] = {kMxTileBytes / 4, groups, mx_bands(rows)}, stride[2] = {kMxTileBytes, groups * kMxTileBytes};
+    const cuuint32_t box[3] = {kMxTileBytes / 4, 2, (cuuint32_t)bands}, step[3] = {1, 1, 1};
+    return g_product_encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void*>(scales), size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 struct Sides {
     const void *r_codes, *c_codes;
     size_t rows, cols;
 };
+constexpr size_t up(size_t n, size_t per) { return (n + per - 1) / per; }
 
-template <int BN, int STAGES, bool SPLIT>
-int launch_product(const Sides& sides, Product k, unsigned parts, unsigned most_ctas, cudaStream_t st)
+bool set_tiles(Product& k, const Sides& s, int row_tile, int col_tile)
 {
-    CUtensorMap r_map, c_map;
-    if (!operand_map(&r_map, sides.r_codes, sides.rows, k.depth_blocks, kRows) || !operand_map(&c_map, sides.c_codes, sides.cols, k.depth_blocks, BN)) return ZCCL_E_CUDA;
-    k.row_tiles = (uint32_t)((sides.rows + kRows - 1) / kRows);
-    k.col_tiles = (uint32_t)((sides.cols + BN - 1) / BN);
-    const unsigned long long total = (unsigned long long)k.row_tiles * k.col_tiles;
-    if (total * parts > 0x7FFFFFFFu) return ZCCL_E_ARG;
-    const unsigned ctas = SPLIT ? (unsigned)total * parts : (unsigned)std::min<unsigned long long>(total, most_ctas);
-    const cudaError_t e = launch_cluster(parts, mx4_product_kernel<BN, STAGES, SPLIT>, dim3(ctas), dim3(kProductThreads), product_smem<BN, STAGES, SPLIT>(), st, r_map, c_map, k);
+    k.row_tiles = (uint32_t)up(s.rows, row_tile);
+    k.col_tiles = (uint32_t)up(s.cols, col_tile);
+    return (size_t)k.row_tiles * k.col_tiles <= 0x7FFFFFFFu / 16;
+}
+int launched(cudaError_t e)
+{
     if (e == cudaSuccess) count_launches(1);
     return e == cudaSuccess ? ZCCL_OK : ZCCL_E_CUDA;
+}
+template <int BN>
+int launch_split(const Sides& s, Product k, unsigned parts, cudaStream_t st)
+{
+    CUtensorMap r, c;
+    if (!set_tiles(k, s, kRows, BN)) return ZCCL_E_ARG;
+    if (!operand_map(&r, s.r_codes, s.rows, k.depth_blocks, kRows) || !operand_map(&c, s.c_codes, s.cols, k.depth_blocks, BN)) return ZCCL_E_CUDA;
+    return launched(launch_cluster(parts, mx4_split_kernel<BN>, dim3(k.row_tiles * k.col_tiles * parts), dim3(kProductThreads), SplitShape<BN>::kBytes, st, r, c, k));
+}
+template <int BN>
+int launch_pair(const Sides& s, Product k, int pairs, cudaStream_t st)
+{
+    CUtensorMap r, c, rs, cs;
+    if (!set_tiles(k, s, 2 * kRows, BN)) return ZCCL_E_ARG;
+    if (!operand_map(&r, s.r_codes, s.rows, k.depth_blocks, kRows) || !operand_map(&c, s.c_codes, s.cols, k.depth_blocks, BN / 2) ||
+        !scales_map(&rs, k.r_scales, s.rows, k.depth_blocks, 1) || !scales_map(&cs, k.c_scales, s.cols, k.depth_blocks, PairShape<BN>::kBands)) return ZCCL_E_CUDA;
+    const unsigned clusters = std::min(k.row_tiles * k.col_tiles, (unsigned)pairs);
+    return launched(launch_cluster(2, mx4_pair_kernel<BN>, dim3(2 * clusters), dim3(kProductThreads), PairShape<BN>::kBytes, st, r, c, rs, cs, k));
 }
 
 bool aligned16(const void* p) { return p && ((uintptr_t)p & 15u) == 0; }
@@ -372,39 +551,34 @@ int zccl_mx4_matmul(const void* a_codes, const void* a_scales, size_t m, const v
     p.y = y;
     p.pitch = pitch;
     p.type = type;
+    p.wide = (uintptr_t)y % 16 == 0 && pitch * element % 16 == 0;
     p.depth_blocks = (uint32_t)mx_blocks(k);
-    // the longer side goes along the lanes
-    const bool across = m < n && m <= 128;
+    // few rows of the output go along the instruction's columns, the weights along its lanes
     Sides sides{a_codes, b_codes, m, n};
     p.r_scales = (const unsigned char*)a_scales;
     p.c_scales = (const unsigned char*)b_scales;
-    if (across) {
+    p.across = m < n && m <= 128;
+    if (p.across) {
         std::swap(sides.r_codes, sides.c_codes);
         std::swap(sides.rows, sides.cols);
         std::swap(p.r_scales, p.c_scales);
     }
-    p.across = across;
     p.rows = (uint32_t)sides.rows;
     p.cols = (uint32_t)sides.cols;
-    const unsigned sms = (unsigned)dev->sms;
-    const uint32_t depth_tiles = (p.depth_blocks + 7) / 8;
-    const size_t row_tiles = (sides.rows + kRows - 1) / kRows;
-    if (sides.cols <= 128) {
-        unsigned parts = 1;
-        while (parts < 8 && parts * 2 <= depth_tiles && row_tiles * parts * 2 <= 2 * sms) parts *= 2;
-        if (sides.cols <= 16) return launch_product<16, 4, true>(sides, p, parts, 0, st);
-        if (sides.cols <= 32) return launch_product<32, 4, true>(sides, p, parts, 0, st);
-        if (sides.cols <= 64) return launch_product<64, 4, true>(sides, p, parts, 0, st);
-        return launch_product<128, 3, true>(sides, p, parts, 0, st);
-    }
-    const size_t tiles = row_tiles * ((sides.cols + 127) / 128);
-    if (tiles * 2 <= sms) {
+    const size_t sms = (size_t)dev->sms, depth_tiles = up(p.depth_blocks, 8), tiles = up(sides.rows, kRows) * up(sides.cols, 128);
+    if (tiles <= sms || sides.cols <= 128) {
+        // the contraction in as many pieces as the SMs take at two to an SM
         unsigned parts = 1;
         while (parts < 8 && parts * 2 <= depth_tiles && tiles * parts * 2 <= 2 * sms) parts *= 2;
-        if (parts > 1) return launch_product<128, 3, true>(sides, p, parts, 0, st);
+        if (sides.cols <= 16) return launch_split<16>(sides, p, parts, st);
+        if (sides.cols <= 32) return launch_split<32>(sides, p, parts, st);
+        if (sides.cols <= 64) return launch_split<64>(sides, p, parts, st);
+        return launch_split<128>(sides, p, parts, st);
     }
-    if (row_tiles * ((sides.cols + 191) / 192) >= sms) return launch_product<192, 5, false>(sides, p, 1, sms, st);
-    return launch_product<128, 6, false>(sides, p, 1, sms, st);
+    // whichever is through in less: a round of tiles half as wide takes a little more than half as long
+    const size_t pairs = (size_t)dev->pairs, rounds_256 = up(up(sides.rows, 256) * up(sides.cols, 256), pairs), rounds_128 = up(up(sides.rows, 256) * up(sides.cols, 128), pairs);
+    if (rounds_256 * 16 <= rounds_128 * 9) return launch_pair<256>(sides, p, dev->pairs, st);
+    return launch_pair<128>(sides, p, dev->pairs, st);
 }
 
 int zccl_mx4_status(void* stream)

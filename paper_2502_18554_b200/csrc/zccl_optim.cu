@@ -15,10 +15,11 @@ namespace {
 constexpr int kOptThreads = 256;
 constexpr int kPerThread = 8;                       // neighbouring elements of a thread: four threads hold a block of 32
 constexpr int kPass = kOptThreads * kPerThread;
-constexpr int kChunk = 4 * kPass;                   // elements of a tensor that a CTA takes
+constexpr int kChunk = 4 * kPass;                   // elements of a gradient that a CTA takes the norm of at a time
+constexpr int kChunksWanted = 1024;                 // of a step, before they get longer
 // Tensors travel as kernel arguments, so a call copies nothing, needs no memory and can be captured.  Arguments above 4 KB cost
 // the launch a few microseconds, hence two sizes of the list.
-constexpr int kFewTensors = 40, kManyTensors = 380;
+constexpr int kFewTensors = 40, kManyTensors = 360;
 
 // Which tensor chunk `c` belongs to: the last one that begins at or in front of it (tensors without elements have no chunks).
 template <class L>
@@ -35,20 +36,48 @@ __device__ __forceinline__ int tensor_of(const L& list, uint32_t c)
 template <class T>
 __device__ __forceinline__ bool wide(const T* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Eight neighbouring elements as they are in memory.
+template <class T> struct Eight { uint4 w[sizeof(T) / 2]; };
+
+template <class T>
+__device__ __forceinline__ Eight<T> load_wide(const T* p)
+{
+    Eight<T> e;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+    return e;
+}
+template <class T>
+__device__ __forceinline__ void values_of(const Eight<T>& e, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = mx_float(reinterpret_cast<const T*>(e.w)[i]);
+}
+__device__ __forceinline__ uint32_t two_of(float a, float b, __nv_bfloat16)
+{
+    const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&p);
+}
+__device__ __forceinline__ uint32_t two_of(float a, float b, __half)
+{
+    const __half2 p = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&p);
+}
+template <class T>
+__device__ __forceinline__ void store_wide(T* p, const float (&v)[8])
+{
+    uint4* const out = reinterpret_cast<uint4*>(p);
+    if constexpr (sizeof(T) == 4) {
+        __stcs(out, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
+        __stcs(out + 1, make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
+    } else __stcs(out, make_uint4(two_of(v[0], v[1], T()), two_of(v[2], v[3], T()), two_of(v[4], v[5], T()), two_of(v[6], v[7], T())));
+}
 // `full`: all eight are there and the array begins on a 16-byte boundary; else the first `left` ones are read.
 template <class T>
 __device__ __forceinline__ void read8(const T* p, bool full, int left, float (&v)[8])
 {
-    constexpr int kPer = 16 / sizeof(T);
-    if (full) {
-#pragma unroll
-        for (int i = 0; i < 8 / kPer; ++i) {
-            const uint4 raw = __ldcs(reinterpret_cast<const uint4*>(p) + i);
-            const MxPack<T> pack = *reinterpret_cast<const MxPack<T>*>(&raw);
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) v[kPer * i + j] = mx_float(pack.v[j]);
-        }
-    } else {
+    if (full) values_of(load_wide(p), v);
+    else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i < left ? mx_float(p[i]) : 0.0f;
     }
@@ -56,16 +85,8 @@ __device__ __forceinline__ void read8(const T* p, bool full, int left, float (&v
 template <class T>
 __device__ __forceinline__ void write8(T* p, bool full, int left, const float (&v)[8])
 {
-    constexpr int kPer = 16 / sizeof(T);
-    if (full) {
-#pragma unroll
-        for (int i = 0; i < 8 / kPer; ++i) {
-            MxPack<T> pack;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) pack.v[j] = mx_round<T>(v[kPer * i + j]);
-            __stcs(reinterpret_cast<uint4*>(p) + i, *reinterpret_cast<const uint4*>(&pack));
-        }
-    } else {
+    if (full) store_wide(p, v);
+    else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < left) p[i] = mx_round<T>(v[i]);
@@ -76,11 +97,11 @@ __device__ __forceinline__ void write8(T* p, bool full, int left, const float (&
 
 constexpr int kNormCtas = 1024;   // partial sums of a launch
 
+template <int CAP>
 struct NormList {
-    static constexpr int kMost = kManyTensors;
-    const void* g[kMost];
-    unsigned long long n[kMost];
-    uint32_t first[kMost];
+    const void* g[CAP];
+    unsigned long long n[CAP];
+    uint32_t first[CAP];
     uint32_t chunks;
     int count;
 };
@@ -101,8 +122,19 @@ __device__ __forceinline__ double block_sum(double s)
 // A thread squares and adds the eight elements that it holds in binary32 and all that follows in binary64: converting every element
 // would cost the double-precision units more than the memory has time for.  Where the eight's sum may have left the range
 // of binary32 it is taken again in binary64.
-template <class G>
-__global__ void __launch_bounds__(kOptThreads) norm_parts_kernel(const __grid_constant__ NormList list, double* __restrict__ parts)
+__device__ __forceinline__ double squares_of(const float (&v)[8])
+{
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = __fmaf_rn(v[j], v[j], s);
+    if (s > 1e-24f && s < 1e37f) return (double)s;
+    double d = 0.0;
+    for (int j = 0; j < 8; ++j) d += (double)v[j] * (double)v[j];
+    return d;
+}
+// `norm`: given to a launch of one CTA that has everything; else the sums of all CTAs are left to norm_join_kernel.
+template <class G, int CAP>
+__global__ void __launch_bounds__(kOptThreads) norm_parts_kernel(const __grid_constant__ NormList<CAP> list, double* __restrict__ parts, float* __restrict__ norm)
 {
     pdl_enter();
     double sum = 0.0;
@@ -112,23 +144,29 @@ __global__ void __launch_bounds__(kOptThreads) norm_parts_kernel(const __grid_co
         const G* g = (const G*)list.g[t] + begin;
         const bool aligned = wide((const G*)list.g[t]);
         const int left_all = (int)min((unsigned long long)kChunk, n - begin);
+        if (aligned && left_all == kChunk) {
+            Eight<G> e[kChunk / kPass];
 #pragma unroll
-        for (int i = 0; i < kChunk / kPass; ++i) {
-            const int at = i * kPass + threadIdx.x * kPerThread, left = left_all - at;
-            if (left > 0) {
+            for (int i = 0; i < kChunk / kPass; ++i) e[i] = load_wide(g + i * kPass + threadIdx.x * kPerThread);
+#pragma unroll
+            for (int i = 0; i < kChunk / kPass; ++i) {
                 float v[8];
-                read8(g + at, aligned && left >= 8, left, v);
-                float s = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) s = __fmaf_rn(v[j], v[j], s);
-                if (s > 1e-24f && s < 1e37f) sum += (double)s;
-                else
-                    for (int j = 0; j < 8; ++j) sum += (double)v[j] * (double)v[j];
+                values_of(e[i], v);
+                sum += squares_of(v);
+            }
+        } else {
+            for (int at = threadIdx.x * kPerThread; at < left_all; at += kPass) {
+                float v[8];
+                read8(g + at, aligned && left_all - at >= 8, left_all - at, v);
+                sum += squares_of(v);
             }
         }
     }
     sum = block_sum(sum);
-    if (threadIdx.x == 0) parts[blockIdx.x] = sum;
+    if (threadIdx.x == 0) {
+        if (norm) *norm = (float)sqrt(sum);
+        else parts[blockIdx.x] = sum;
+    }
 }
 
 __global__ void __launch_bounds__(kOptThreads) norm_join_kernel(const double* __restrict__ parts, uint32_t count, float* __restrict__ norm)
@@ -149,6 +187,7 @@ struct AdamTensor {
     unsigned char *m_scale, *v_scale;
     void* copy;
     unsigned long long n, place;   // `place`: its first element in the order that the random bits go by
+    bool wide;                     // all arrays begin on 16-byte boundaries
 };
 template <int CAP>
 struct AdamList {
@@ -158,7 +197,8 @@ struct AdamList {
 };
 
 struct AdamCall {
-    float beta1, rest1, beta2, rest2, eps;
+    float beta1, rest1, beta2, eps;
+    float root_beta2, root_rest2;  // square roots of beta2 and of 1 - beta2
     float keep, rate, root;        // 1 - lr weight_decay; lr / (1 - beta1^step); 1 / sqrt(1 - beta2^step)
     double lr, weight_decay, log_beta1, log_beta2;   // where step or lr is on the device
     const long long* step;
@@ -168,26 +208,36 @@ struct AdamCall {
     const float* norm;
     float max_norm;
     int copy_type;
+    uint32_t passes;               // of 2048 elements to a chunk
 };
 
 __host__ __device__ inline unsigned long long random_key(unsigned long long seed, long long step)
 {
     return seed + (unsigned long long)step * 0x9E3779B97F4A7C15ull;
 }
-// 32 random bits for the element at `place`: three rounds of multiplying and folding the upper bits down.
-__device__ __forceinline__ uint32_t random_bits(unsigned long long key, unsigned long long place)
+// 32 random bits h for the element at `place`: three rounds of multiplying and folding the upper bits down, the last fold left to noise_of.
+// `low` is the lower half of place ^ key, `high` the upper half of place ^ key.
+__device__ __forceinline__ uint32_t random_bits(uint32_t low, uint32_t high)
 {
-    uint32_t h = ((uint32_t)place ^ (uint32_t)key) * 0x7FEB352Du;
-    h = ((h ^ (h >> 15)) ^ (uint32_t)(key >> 32) ^ (uint32_t)(place >> 32)) * 0x846CA68Bu;
-    h = (h ^ (h >> 13)) * 0x6C8E9CF5u;
-    return h ^ (h >> 16);
+    uint32_t h = low * 0x7FEB352Du;
+    h = ((h ^ (h >> 15)) ^ high) * 0x846CA68Bu;
+    return (h ^ (h >> 13)) * 0x6C8E9CF5u;
+}
+// The upper 16 of the bits h ^ (h >> 16), and the lower 16, each in bits 8 ... 23.
+__device__ __forceinline__ void noise_of(uint32_t h, uint32_t& first, uint32_t& second)
+{
+    first = prmt(h, 0, 0x4324);
+    second = prmt(h, 0, 0x4104) ^ first;
 }
 
+// The largest magnitude of a block, as bits, of which four neighbouring lanes hold eight each.
+template <bool ROOT>
 __device__ __forceinline__ uint32_t top8(const float (&v)[8])
 {
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    for (int i = 0; i < 8; ++i) top = max(top, ROOT ? __float_as_uint(v[i]) : __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    if (ROOT) top &= 0x7FFFFFFFu;                    // roots are not negative; a NaN may have a sign
     top = max(top, __shfl_xor_sync(kFull, top, 1));
     return max(top, __shfl_xor_sync(kFull, top, 2));
 }
@@ -197,24 +247,16 @@ __device__ __forceinline__ uint32_t exponent8(uint32_t top)
     const int field = (int)(top >> 23);
     return field == 255 ? 255u : (uint32_t)max(field - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0), 0);
 }
-// One value, already times 2^-e, to E4M3: `noise` (20 bits) is added below the last bit that is kept.  Magnitudes below 2^-6 have the
-// step of 2^-9: with 2^-6 added their step is where a normal number's is.
-__device__ __forceinline__ uint32_t encode8(float y, uint32_t noise)
-{
-    const float a = fabsf(y);
-    const bool small = a < 0.015625f;
-    const float b = small ? __fadd_rz(a, 0.015625f) : a;
-    return ((__float_as_uint(b) + noise) >> 20) - (small ? 968u : 960u);
-}
-__device__ __forceinline__ void decode8(uint2 w, float scale, float (&v)[8])
+// Eight codes as the numbers that E4M3 gives them (without the block's scale).
+__device__ __forceinline__ void decode8(uint2 w, float (&v)[8])
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t two = (i & 2 ? w.y : w.x) >> (16 * (i & 1));
         const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(two & 0xFFFFu), __NV_E4M3);
         const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-        v[2 * i] = f.x * scale;
-        v[2 * i + 1] = f.y * scale;
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
     }
 }
 __device__ __forceinline__ uint2 read_codes(const unsigned char* p, bool full, int left)
@@ -235,32 +277,87 @@ __device__ __forceinline__ void write_codes(unsigned char* p, bool full, int lef
             if (i < left) p[i] = (unsigned char)((i & 4 ? w.y : w.x) >> (8 * (i & 3)));
     }
 }
-// Eight elements of a block to codes; `shift` says which half of the random bits they take.
+// Eight elements of a block to codes with the block's biased exponent s.  Times 2^-120 a magnitude's bits in binary32 are E4M3's, 20 places further
+// up, subnormal numbers of the one among those of the other, so rounding is one addition below the last bit that is kept: `noise` has its
+// 16 random bits in bits 8 ... 23, the magnitude is moved up by four to meet them, and the code is the top byte.
 template <bool ROOT>
-__device__ __forceinline__ uint2 pack8(const float (&v)[8], const uint32_t (&random)[8], uint32_t s)
+__device__ __forceinline__ uint2 pack8(float (&v)[8], const uint32_t (&noise)[8], uint32_t s)
 {
-    const float inverse = __uint_as_float((254u - s) << 23);
-    uint32_t w[2] = {0, 0};
+    if (s > 133u) {                                  // 2^-e 2^-120 would be no normal number: in two steps
+        const float down = __uint_as_float((254u - min(s, 253u)) << 23);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= down;
+        if (s == 255u) return make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
+        s = 127u;
+    }
+    const float inverse = __uint_as_float((134u - s) << 23);
+    uint32_t z[8], least = 0xFFFFFFFFu;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint32_t noise = ROOT ? (random[i] & 0xFFFFu) << 4 : random[i] >> 16 << 4;
-        uint32_t c = encode8(v[i] * inverse, noise);
-        if (ROOT) c = max(c, v[i] > 0.0f ? 1u : 0u);
-        else c |= __float_as_uint(v[i]) >> 31 << 7;
-        w[i >> 2] |= c << (8 * (i & 3));
+        const uint32_t bits = __float_as_uint(v[i] * inverse);
+        z[i] = (bits << 4) + noise[i];
+        if (ROOT) least = min(least, z[i]);
+        else z[i] |= bits & 0x80000000u;
     }
-    return s == 255u ? make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu) : make_uint2(w[0], w[1]);
+    if (ROOT && least < 0x01000000u) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = max(z[i], v[i] > 0.0f ? 0x01000000u : 0u);
+    }
+    return make_uint2(prmt(prmt(z[0], z[1], 0x0073), prmt(z[2], z[3], 0x0073), 0x5410), prmt(prmt(z[4], z[5], 0x0073), prmt(z[6], z[7], 0x0073), 0x5410));
 }
 
+// Both to within 2^-22; subnormal numbers count as zero.
 __device__ __forceinline__ float root_of(float v)
 {
     float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float reciprocal_of(float v)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
 
+// What a step does to an element, with everything that does not depend on it worked out before.
+struct AdamRates {
+    float keep, rate, root;        // see AdamCall
+    float gain1, gain2;            // what a gradient enters m with, and the root of what its square enters v with (clipping included)
+    unsigned long long key;
+};
+
+template <bool EIGHT>
+__device__ __forceinline__ void update8(const AdamCall& call, const AdamRates& k, float m_unit, float v_unit, const float (&g)[8], float (&p)[8], float (&m)[8], float (&v)[8], float (&r)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        m[i] = __fmaf_rn(k.gain1, g[i], m_unit * m[i]);
+        const float u = k.gain2 * g[i], w = v_unit * v[i];
+        v[i] = __fmaf_rn(u, u, EIGHT ? w * w : w);
+        r[i] = root_of(v[i]);
+        p[i] = __fmaf_rn(-k.rate, m[i] * reciprocal_of(__fmaf_rn(r[i], k.root, call.eps)), p[i] * k.keep);
+    }
+}
+// New states of eight elements to codes; `place` counts the first one.
+__device__ __forceinline__ void encode_states(const AdamRates& k, unsigned long long place, float (&m)[8], float (&r)[8], uint2& mc, uint2& vc, uint32_t& ms, uint32_t& vs)
+{
+    const unsigned long long from = place ^ k.key;   // `place` is a multiple of 8: element i changes the lowest bits alone
+    uint32_t first[8], second[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) noise_of(random_bits((uint32_t)from ^ i, (uint32_t)(from >> 32)), first[i], second[i]);
+    ms = exponent8(top8<false>(m));
+    vs = exponent8(top8<true>(r));
+    mc = pack8<false>(m, first, ms);
+    vc = pack8<true>(r, second, vs);
+}
+
+// A CTA takes a chunk of `passes` times 2048 elements of one tensor, a thread eight neighbours at a time.  Chunks that are whole, of arrays on
+// 16-byte boundaries, go the short way, where the next eight are loaded while these are worked on.  States in 32 bits: bound by memory, two CTAs to an SM
+// have enough loads in flight.  In 8 bits: about 50 instructions to an element against 10 bytes, so issue and memory take about as long and warps have
+// to cover each other's waits: four CTAs, though a few registers are spilled for it (128 Mi bf16 parameters: 261 us, with two or three CTAs 335).
 template <class P, class G, bool EIGHT, int CAP>
-__global__ void __launch_bounds__(kOptThreads) adamw_kernel(const __grid_constant__ AdamList<CAP> list, const __grid_constant__ AdamCall call)
+__global__ void __launch_bounds__(kOptThreads, EIGHT ? 4 : 2) adamw_kernel(const __grid_constant__ AdamList<CAP> list, const __grid_constant__ AdamCall call)
 {
     pdl_enter();
     float clip = 1.0f;
@@ -269,12 +366,11 @@ __global__ void __launch_bounds__(kOptThreads) adamw_kernel(const __grid_constan
         if (!(norm >= 0.0f && norm < __int_as_float(0x7F800000))) return;   // no norm of finite gradients: no step
         clip = fminf(1.0f, __fdiv_rn(call.max_norm, norm + 1e-6f));
     }
-    float keep = call.keep, rate = call.rate, root = call.root;
-    unsigned long long key = random_key(call.seed, call.step_host);
+    AdamRates k{call.keep, call.rate, call.root, call.rest1 * clip, call.root_rest2 * clip, random_key(call.seed, call.step_host)};
     if (call.step || call.lr_device) {
         __shared__ float sh[3];
         const long long step = call.step ? *call.step : call.step_host;
-        key = random_key(call.seed, step);
+        k.key = random_key(call.seed, step);
         if (threadIdx.x == 0) {
             const double lr = call.lr_device ? (double)*call.lr_device : call.lr;
             sh[0] = (float)(1.0 - lr * call.weight_decay);
@@ -282,18 +378,94 @@ __global__ void __launch_bounds__(kOptThreads) adamw_kernel(const __grid_constan
             sh[2] = (float)(1.0 / sqrt(-expm1((double)step * call.log_beta2)));
         }
         __syncthreads();
-        keep = sh[0];
-        rate = sh[1];
-        root = sh[2];
+        k.keep = sh[0];
+        k.rate = sh[1];
+        k.root = sh[2];
     }
     const int t = tensor_of(list, blockIdx.x);
     const AdamTensor& a = list.t[t];
-    const unsigned long long begin = (unsigned long long)(blockIdx.x - list.first[t]) * kChunk;
-    const int left_all = (int)min((unsigned long long)kChunk, a.n - begin);
+    const uint32_t chunk = call.passes * kPass;
+    const unsigned long long begin = (unsigned long long)(blockIdx.x - list.first[t]) * chunk;
+    const uint32_t mine = threadIdx.x * kPerThread;
+    if (a.wide && a.n - begin >= chunk) {
+        P* p = (P*)a.p + begin + mine;
+        const G* g = (const G*)a.g + begin + mine;
+        unsigned char* copy = a.copy ? (unsigned char*)a.copy + 2 * (begin + mine) : nullptr;
+        unsigned long long place = a.place + begin + mine;
+        Eight<P> pe = load_wide(p);
+        Eight<G> ge = load_wide(g);
+        if (EIGHT) {
+            unsigned char *mc = (unsigned char*)a.m + begin + mine, *vc = (unsigned char*)a.v + begin + mine;
+            unsigned char *ms = a.m_scale + (begin + mine) / kMxBlock, *vs = a.v_scale + (begin + mine) / kMxBlock;
+            uint2 me = __ldcs(reinterpret_cast<const uint2*>(mc)), ve = __ldcs(reinterpret_cast<const uint2*>(vc));
+            uint32_t mu = *ms, vu = *vs;
+            for (uint32_t i = 1; i <= call.passes; ++i) {
+                float pv[8], gv[8], mv[8], vv[8], rv[8];
+                values_of(pe, pv);
+                values_of(ge, gv);
+                decode8(me, mv);
+                decode8(ve, vv);
+                const float m_unit = call.beta1 * mx_scale(mu), v_unit = call.root_beta2 * mx_scale(vu);
+                if (i < call.passes) {
+                    pe = load_wide(p + kPass);
+                    ge = load_wide(g + kPass);
+                    me = __ldcs(reinterpret_cast<const uint2*>(mc + kPass));
+                    ve = __ldcs(reinterpret_cast<const uint2*>(vc + kPass));
+                    mu = ms[kPass / kMxBlock];
+                    vu = vs[kPass / kMxBlock];
+                }
+                update8<true>(call, k, m_unit, v_unit, gv, pv, mv, vv, rv);
+                store_wide(p, pv);
+                if (copy) {
+                    if (call.copy_type == ZCCL_BF16) store_wide((__nv_bfloat16*)copy, pv);
+                    else store_wide((__half*)copy, pv);
+                    copy += 2 * kPass;
+                }
+                uint2 mw, vw;
+                uint32_t se, re;
+                encode_states(k, place, mv, rv, mw, vw, se, re);
+                __stcs(reinterpret_cast<uint2*>(mc), mw);
+                __stcs(reinterpret_cast<uint2*>(vc), vw);
+                if ((threadIdx.x & 3) == 0) {
+                    *ms = (unsigned char)se;
+                    *vs = (unsigned char)re;
+                }
+                p += kPass; g += kPass; mc += kPass; vc += kPass; ms += kPass / kMxBlock; vs += kPass / kMxBlock; place += kPass;
+            }
+        } else {
+            float *m = (float*)a.m + begin + mine, *v = (float*)a.v + begin + mine;
+            Eight<float> me = load_wide(m), ve = load_wide(v);
+            for (uint32_t i = 1; i <= call.passes; ++i) {
+                float pv[8], gv[8], mv[8], vv[8], rv[8];
+                values_of(pe, pv);
+                values_of(ge, gv);
+                values_of(me, mv);
+                values_of(ve, vv);
+                update8<false>(call, k, call.beta1, call.beta2, gv, pv, mv, vv, rv);
+                if (i < call.passes) {
+                    pe = load_wide(p + kPass);
+                    ge = load_wide(g + kPass);
+                    me = load_wide((const float*)m + kPass);
+                    ve = load_wide((const float*)v + kPass);
+                }
+                store_wide(p, pv);
+                if (copy) {
+                    if (call.copy_type == ZCCL_BF16) store_wide((__nv_bfloat16*)copy, pv);
+                    else store_wide((__half*)copy, pv);
+                    copy += 2 * kPass;
+                }
+                store_wide(m, mv);
+                store_wide(v, vv);
+                p += kPass; g += kPass; m += kPass; v += kPass;
+            }
+        }
+        return;
+    }
+    const int left_all = (int)min((unsigned long long)chunk, a.n - begin);
     P* const p = (P*)a.p + begin;
     const G* const g = (const G*)a.g + begin;
     const bool p_wide = wide(p), g_wide = wide(g), copies = a.copy != nullptr, copy_wide = wide((const __half*)a.copy);
-    for (int at = threadIdx.x * kPerThread; at - (int)(threadIdx.x & 31) * kPerThread < left_all; at += kPass) {   // whole warps
+    for (int at = mine; at - (int)(threadIdx.x & 31) * kPerThread < left_all; at += kPass) {   // whole warps
         const int left = left_all - at;
         const bool all = left >= 8;
         float pv[8], gv[8], mv[8], vv[8], rv[8];
@@ -301,6 +473,7 @@ __global__ void __launch_bounds__(kOptThreads) adamw_kernel(const __grid_constan
         read8(g + at, all && g_wide, left, gv);
         unsigned char *mc = nullptr, *vc = nullptr, *ms = nullptr, *vs = nullptr;
         bool m_wide, v_wide;
+        float m_unit = call.beta1, v_unit = call.beta2;
         if (EIGHT) {
             mc = (unsigned char*)a.m + begin + at;
             vc = (unsigned char*)a.v + begin + at;
@@ -308,39 +481,33 @@ __global__ void __launch_bounds__(kOptThreads) adamw_kernel(const __grid_constan
             vs = a.v_scale + (begin + at) / kMxBlock;
             m_wide = all && ((uintptr_t)mc & 7u) == 0;
             v_wide = all && ((uintptr_t)vc & 7u) == 0;
-            decode8(read_codes(mc, m_wide, left), mx_scale(left > 0 ? *ms : 0u), mv);
-            decode8(read_codes(vc, v_wide, left), mx_scale(left > 0 ? *vs : 0u), vv);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) vv[i] *= vv[i];
+            m_unit = call.beta1 * mx_scale(left > 0 ? *ms : 0u);
+            v_unit = call.root_beta2 * mx_scale(left > 0 ? *vs : 0u);
+            decode8(read_codes(mc, m_wide, left), mv);
+            decode8(read_codes(vc, v_wide, left), vv);
         } else {
             m_wide = all && wide((float*)a.m);
             v_wide = all && wide((float*)a.v);
             read8((const float*)a.m + begin + at, m_wide, left, mv);
             read8((const float*)a.v + begin + at, v_wide, left, vv);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float gc = gv[i] * clip;
-            mv[i] = __fmaf_rn(call.rest1, gc, call.beta1 * mv[i]);
-            vv[i] = __fmaf_rn(call.rest2 * gc, gc, call.beta2 * vv[i]);
-            rv[i] = root_of(vv[i]);
-            pv[i] = __fmaf_rn(pv[i], keep, -(rate * __fdividef(mv[i], __fmaf_rn(rv[i], root, call.eps))));
-        }
+        update8<EIGHT>(call, k, m_unit, v_unit, gv, pv, mv, vv, rv);
         write8(p + at, all && p_wide, left, pv);
         if (copies) {
             if (call.copy_type == ZCCL_BF16) write8((__nv_bfloat16*)a.copy + begin + at, all && copy_wide, left, pv);
             else write8((__half*)a.copy + begin + at, all && copy_wide, left, pv);
         }
         if (EIGHT) {
-            uint32_t random[8];
+            if (!all) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                random[i] = random_bits(key, a.place + begin + at + i);
-                if (i >= left) mv[i] = rv[i] = 0.0f;
+                for (int i = 0; i < 8; ++i)
+                    if (i >= left) mv[i] = rv[i] = 0.0f;
             }
-            const uint32_t se = exponent8(top8(mv)), re = exponent8(top8(rv));
-            write_codes(mc, m_wide, left, pack8<false>(mv, random, se));
-            write_codes(vc, v_wide, left, pack8<true>(rv, random, re));
+            uint2 mw, vw;
+            uint32_t se, re;
+            encode_states(k, a.place + begin + at, mv, rv, mw, vw, se, re);
+            write_codes(mc, m_wide, left, mw);
+            write_codes(vc, v_wide, left, vw);
             if ((threadIdx.x & 3) == 0 && left > 0) {
                 *ms = (unsigned char)se;
                 *vs = (unsigned char)re;
@@ -382,7 +549,7 @@ constexpr uint32_t kMostChunks = 0x7FFFFFFFu;
 
 // The list of tensors from `at` on that one launch takes; returns how many entries of `tensors` that covers.
 template <int CAP>
-size_t fill_list(AdamList<CAP>& list, uint32_t& chunks, const zccl_adamw_tensor* tensors, size_t count, size_t at, unsigned long long& place)
+size_t fill_list(AdamList<CAP>& list, uint32_t& chunks, const zccl_adamw_tensor* tensors, size_t count, size_t at, unsigned long long& place, size_t chunk)
 {
     list.count = 0;
     chunks = 0;
@@ -390,9 +557,11 @@ size_t fill_list(AdamList<CAP>& list, uint32_t& chunks, const zccl_adamw_tensor*
     for (; i < count && list.count < CAP; ++i) {
         const zccl_adamw_tensor& s = tensors[i];
         if (s.n == 0) continue;
-        const size_t mine = (s.n + kChunk - 1) / kChunk;
+        const size_t mine = (s.n + chunk - 1) / chunk;
         if (mine > kMostChunks - chunks) break;
-        list.t[list.count] = {s.p, s.g, s.m, s.v, (unsigned char*)s.m_scale, (unsigned char*)s.v_scale, s.copy, s.n, place};
+        AdamTensor& to = list.t[list.count];
+        to = {s.p, s.g, s.m, s.v, (unsigned char*)s.m_scale, (unsigned char*)s.v_scale, s.copy, s.n, place, false};
+        to.wide = (((uintptr_t)s.p | (uintptr_t)s.g | (uintptr_t)s.m | (uintptr_t)s.v | (uintptr_t)s.copy) % 16) == 0;
         list.first[list.count++] = chunks;
         chunks += (uint32_t)mine;
         place += (s.n + kMxBlock - 1) / kMxBlock * kMxBlock;
@@ -408,13 +577,53 @@ int run_list(const zccl_adamw_tensor* tensors, size_t count, const zccl_adamw_co
     int rc = ZCCL_OK;
     for (size_t at = 0; at < count && rc == ZCCL_OK;) {
         uint32_t chunks;
-        at += fill_list(*list, chunks, tensors, count, at, place);
+        at += fill_list(*list, chunks, tensors, count, at, place, (size_t)call.passes * kPass);
         if (chunks == 0) continue;
         if (launch_adamw_param(k, *list, chunks, call, st) == cudaSuccess) count_launches(1);
         else rc = ZCCL_E_CUDA;
     }
     delete list;
     return rc;
+}
+
+// Up to this many chunks are one CTA's work in less time than a second launch takes.
+constexpr size_t kNormAlone = 4;
+
+template <int CAP>
+int run_norm(const void* const* g, const size_t* n, size_t count, size_t chunks, int type, float* norm, double* parts, cudaStream_t st)
+{
+    NormList<CAP>* list = new (std::nothrow) NormList<CAP>;
+    if (!list) return ZCCL_E_ARG;
+    uint32_t written = 0;
+    cudaError_t e = cudaSuccess;
+    bool joined = false;
+    for (size_t at = 0; at < count && e == cudaSuccess;) {
+        list->count = 0;
+        list->chunks = 0;
+        const size_t from = at;
+        for (; at < count && list->count < CAP; ++at) {
+            if (n[at] == 0) continue;
+            const size_t mine = (n[at] + kChunk - 1) / kChunk;
+            if (mine > kMostChunks - list->chunks) break;
+            list->g[list->count] = g[at];
+            list->n[list->count] = n[at];
+            list->first[list->count++] = list->chunks;
+            list->chunks += (uint32_t)mine;
+        }
+        if (list->chunks == 0) continue;
+        joined = chunks <= kNormAlone && from == 0 && list->chunks == chunks;
+        const uint32_t ctas = joined ? 1u : std::min<uint32_t>(list->chunks, kNormCtas);
+        const auto kernel = type == ZCCL_F32 ? norm_parts_kernel<float, CAP> : type == ZCCL_BF16 ? norm_parts_kernel<__nv_bfloat16, CAP> : norm_parts_kernel<__half, CAP>;
+        e = launch_k(kernel, dim3(ctas), dim3(kOptThreads), 0, st, *list, parts + written, joined ? norm : nullptr);
+        if (e == cudaSuccess) count_launches(1);
+        written += ctas;
+    }
+    delete list;
+    if (!joined && e == cudaSuccess) {
+        e = launch_k(norm_join_kernel, dim3(1), dim3(kOptThreads), 0, st, parts, written, norm);
+        if (e == cudaSuccess) count_launches(1);
+    }
+    return e == cudaSuccess ? ZCCL_OK : ZCCL_E_CUDA;
 }
 
 bool type_ok(int t) { return t >= ZCCL_F32 && t <= ZCCL_F16; }
@@ -437,11 +646,12 @@ int zccl_adamw(const zccl_adamw_tensor* tensors, size_t count, const zccl_adamw_
     if (!rate_ok(k.beta1) || !rate_ok(k.beta2) || !(k.eps >= 0.0) || !std::isfinite(k.eps) || !std::isfinite(k.weight_decay)) return ZCCL_E_ARG;
     if ((!k.lr_device && !std::isfinite(k.lr)) || (!k.step_device && k.step < 1) || (k.norm && !(k.max_norm > 0.0))) return ZCCL_E_ARG;
     if (((uintptr_t)k.step_device & 7u) || ((uintptr_t)k.lr_device & 3u) || ((uintptr_t)k.norm & 3u)) return ZCCL_E_ARG;
-    size_t used = 0;
+    size_t used = 0, total = 0;
     for (size_t i = 0; i < count; ++i) {
         const zccl_adamw_tensor& t = tensors[i];
         if (t.n == 0) continue;
         ++used;
+        total += t.n;
         const uintptr_t state = k.state_bits == 8 ? 0u : 3u;
         if (t.n > kMostElems || !at_element(t.p, mask_of(k.param_type)) || !at_element(t.g, mask_of(k.grad_type)) || !at_element(t.m, state) || !at_element(t.v, state))
             return ZCCL_E_ARG;
@@ -453,7 +663,8 @@ int zccl_adamw(const zccl_adamw_tensor* tensors, size_t count, const zccl_adamw_
     call.beta1 = (float)k.beta1;
     call.rest1 = (float)(1.0 - k.beta1);
     call.beta2 = (float)k.beta2;
-    call.rest2 = (float)(1.0 - k.beta2);
+    call.root_beta2 = (float)std::sqrt(k.beta2);
+    call.root_rest2 = (float)std::sqrt(1.0 - k.beta2);
     call.eps = (float)k.eps;
     call.lr = k.lr;
     call.weight_decay = k.weight_decay;
@@ -471,46 +682,28 @@ int zccl_adamw(const zccl_adamw_tensor* tensors, size_t count, const zccl_adamw_
     call.norm = k.norm;
     call.max_norm = (float)k.max_norm;
     call.copy_type = k.copy_type;
+    // Small models are spread over the SMs; large ones have chunks of up to eight passes, whose first loads alone are not covered by work.
+    call.passes = 1;
+    while (call.passes < 8 && total / kPass > (size_t)kChunksWanted * call.passes) call.passes *= 2;
     return used <= (size_t)kFewTensors ? run_list<kFewTensors>(tensors, count, k, call, (cudaStream_t)stream)
                                        : run_list<kManyTensors>(tensors, count, k, call, (cudaStream_t)stream);
 }
 
-size_t zccl_grad_norm_work(size_t count) { return (count / kManyTensors + 2) * kNormCtas * sizeof(double); }
+size_t zccl_grad_norm_work(size_t count) { return (count / kFewTensors + 2) * kNormCtas * sizeof(double); }
 
 int zccl_grad_norm(const void* const* g, const size_t* n, size_t count, int grad_type, float* norm, void* work, void* stream)
 {
     if (!type_ok(grad_type) || (count && (!g || !n)) || !at_element(norm, 3u) || !at_element(work, 7u)) return ZCCL_E_ARG;
     for (size_t i = 0; i < count; ++i)
         if (n[i] && (n[i] > kMostElems || !at_element(g[i], mask_of(grad_type)))) return ZCCL_E_ARG;
-    NormList* list = new (std::nothrow) NormList;
-    if (!list) return ZCCL_E_ARG;
-    cudaStream_t st = (cudaStream_t)stream;
-    double* parts = (double*)work;
-    uint32_t written = 0;
-    cudaError_t e = cudaSuccess;
-    for (size_t at = 0; at < count && e == cudaSuccess;) {
-        list->count = 0;
-        list->chunks = 0;
-        for (; at < count && list->count < NormList::kMost; ++at) {
-            if (n[at] == 0) continue;
-            const size_t mine = (n[at] + kChunk - 1) / kChunk;
-            if (mine > kMostChunks - list->chunks) break;
-            list->g[list->count] = g[at];
-            list->n[list->count] = n[at];
-            list->first[list->count++] = list->chunks;
-            list->chunks += (uint32_t)mine;
-        }
-        if (list->chunks == 0) continue;
-        const uint32_t ctas = std::min<uint32_t>(list->chunks, kNormCtas);
-        const auto kernel = grad_type == ZCCL_F32 ? norm_parts_kernel<float> : grad_type == ZCCL_BF16 ? norm_parts_kernel<__nv_bfloat16> : norm_parts_kernel<__half>;
-        e = launch_k(kernel, dim3(ctas), dim3(kOptThreads), 0, st, *list, parts + written);
-        if (e == cudaSuccess) count_launches(1);
-        written += ctas;
+    size_t used = 0, chunks = 0;
+    for (size_t i = 0; i < count; ++i) {
+        used += n[i] != 0;
+        chunks += (n[i] + kChunk - 1) / kChunk;
     }
-    delete list;
-    if (e == cudaSuccess) e = launch_k(norm_join_kernel, dim3(1), dim3(kOptThreads), 0, st, parts, written, norm);
-    if (e == cudaSuccess) count_launches(1);
-    return e == cudaSuccess ? ZCCL_OK : ZCCL_E_CUDA;
+    cudaStream_t st = (cudaStream_t)stream;
+    return used <= (size_t)kFewTensors ? run_norm<kFewTensors>(g, n, count, chunks, grad_type, norm, (double*)work, st)
+                                       : run_norm<kManyTensors>(g, n, count, chunks, grad_type, norm, (double*)work, st);
 }
 
 }  // extern "C"

@@ -42,43 +42,38 @@ def empty(rows: int, cols: int, device, stream=None) -> Mx4:
         return Mx4(torch.empty(codes, dtype=torch.uint8, device=device), torch.empty(scales, dtype=torch.uint8, device=device), rows, cols)
 
 
+def _value(r, what: str):
+    """What a native call returned: its result, or a status to raise."""
+    if type(r) is int:
+        z._check(r, what)
+    return r
+
+
 def quantize(x: torch.Tensor, transpose: bool = False, out: Mx4 | None = None, stream=None) -> Mx4:
     """x (float32, bfloat16 or float16 [rows, cols], rows contiguous) in microscaled form, blocks along its rows; with
     `transpose` the form of x's transpose, blocks along x's columns."""
     if x.dim() != 2:
         raise ValueError("expected a matrix")
-    rows, cols = (x.shape[1], x.shape[0]) if transpose else (x.shape[0], x.shape[1])
+    cols, rows = x.shape if transpose else reversed(x.shape)
     if out is None:
-        out = empty(rows, cols, x.device, stream)
-    elif (out.rows, out.cols) != (rows, cols):
+        return Mx4(*_value(z.native().mx4_quantize(x, transpose, None, None, stream), "zccl_mx4_quantize"), rows, cols)
+    if (out.rows, out.cols) != (rows, cols):
         raise ValueError(f"expected the form of a matrix [{rows}, {cols}], got one of [{out.rows}, {out.cols}]")
-    z._check(z.native().mx4_quantize(x, transpose, out.codes, out.scales, stream), "zccl_mx4_quantize")
+    _value(z.native().mx4_quantize(x, transpose, out.codes, out.scales, stream), "zccl_mx4_quantize")
     return out
 
 
 def dequantize(q: Mx4, dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
-    """The values of `q`, each rounded once to `dtype`."""
-    if out is None:
-        with _allocating(stream):
-            out = torch.empty(q.rows, q.cols, dtype=dtype, device=q.codes.device)
-    elif tuple(out.shape) != (q.rows, q.cols):
-        raise ValueError(f"expected an output [{q.rows}, {q.cols}], got {list(out.shape)}")
-    z._check(z.native().mx4_dequantize(q.codes, q.scales, out, stream), "zccl_mx4_dequantize")
-    return out
+    """The values of `q`, each rounded once to `dtype` (or to the type of `out`)."""
+    return _value(z.native().mx4_dequantize(q.codes, q.scales, q.rows, q.cols, dtype, out, stream), "zccl_mx4_dequantize")
 
 
 def matmul(a: Mx4, b: Mx4, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """A B^T of two operands that are quantised along the contraction: a [m, k] and b [n, k] to [m, n], sums in binary32, each
-    rounded once to `dtype` (float32, bfloat16 or float16)."""
+    rounded once to `dtype` (float32, bfloat16 or float16), or to the type of `out`."""
     if a.cols != b.cols:
         raise ValueError(f"operands are contracted over {a.cols} and {b.cols} elements")
-    if out is None:
-        with _allocating(stream):
-            out = torch.empty(a.rows, b.rows, dtype=dtype, device=a.codes.device)
-    elif tuple(out.shape) != (a.rows, b.rows):
-        raise ValueError(f"expected an output [{a.rows}, {b.rows}], got {list(out.shape)}")
-    z._check(z.native().mx4_matmul(a.codes, a.scales, b.codes, b.scales, a.cols, out, stream), "zccl_mx4_matmul")
-    return out
+    return _value(z.native().mx4_matmul(a.codes, a.scales, a.rows, b.codes, b.scales, b.rows, a.cols, dtype, out, stream), "zccl_mx4_matmul")
 
 
 def status(stream=None) -> int:
@@ -90,7 +85,7 @@ class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w):
         ctx.save_for_backward(x, w)
-        return matmul(quantize(x), quantize(w), x.dtype)
+        return _value(z.native().mx4_linear(x, w), "zccl_mx4_matmul")
 
     @staticmethod
     @torch.autograd.function.once_differentiable
@@ -100,23 +95,23 @@ class _Linear(torch.autograd.Function):
 
 
 def linear(x: torch.Tensor, w: torch.Tensor | Mx4) -> torch.Tensor:
-    """x W^T with both sides in microscaled form, in x's type.  x is [..., k]; `w` is [n, k], or already quantised (weights that
-    are laid out once; no gradient then).  With a tensor for `w` this is differentiable, by linear_backward."""
-    rows = x.reshape(-1, x.shape[-1])
+    """x W^T with both sides in microscaled form, in x's type, on the current stream.  x is [..., k]; `w` is [n, k] of x's type, or already
+    quantised (weights that are laid out once; no gradient then).  With a tensor for `w` this is differentiable, by linear_backward."""
+    rows = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
     if isinstance(w, Mx4):
-        if torch.is_grad_enabled() and x.requires_grad:
+        if x.requires_grad and torch.is_grad_enabled():
             raise ValueError("quantised weights are for inference: pass the weights themselves to train, or detach x")
-        y = matmul(quantize(rows), w, x.dtype)
-    else:
-        if w.dtype != x.dtype:
-            raise ValueError(f"x is {x.dtype}, the weights are {w.dtype}")
+        if w.cols != rows.shape[1]:
+            raise ValueError(f"x has rows of {rows.shape[1]}, the weights of {w.cols}")
+        y = _value(z.native().mx4_linear(rows, w.codes, w.scales, w.rows), "zccl_mx4_matmul")
+    elif torch.is_grad_enabled() and (x.requires_grad or w.requires_grad):
         y = _Linear.apply(rows, w)
-    return y.view(*x.shape[:-1], y.shape[-1])
+    else:
+        y = _value(z.native().mx4_linear(rows, w), "zccl_mx4_matmul")
+    return y if x.dim() == 2 else y.view(*x.shape[:-1], y.shape[-1])
 
 
 def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, needed=(True, True)):
     """The gradients of linear(x, w) for matrices, from dy [m, n]: dx = Q(dy) Q(w^T)^T, contracted and quantised along n, and
     dw = Q(dy^T) Q(x^T)^T along m, each in its operand's type (quantisation itself passes gradients on unchanged)."""
-    dx = matmul(quantize(dy), quantize(w, transpose=True), x.dtype) if needed[0] else None
-    dw = matmul(quantize(dy, transpose=True), quantize(x, transpose=True), w.dtype) if needed[1] else None
-    return dx, dw
+    return _value(z.native().mx4_linear_backward(dy, x, w, needed[0], needed[1]), "zccl_mx4_matmul")

@@ -7,22 +7,12 @@ from __future__ import annotations
 import torch
 
 from . import zccl as z
-from .mx import _allocating
-
-BLOCK = 32
+from .mx import _value
 
 
 def grad_norm(grads, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """sqrt(sum of g^2) over all of `grads` (CUDA tensors of one type), as a float32 [1] on their device."""
-    if out is None:
-        if not len(grads):
-            raise ValueError("no gradients to take a device from: pass `out`")
-        with _allocating(stream):
-            out = torch.empty(1, dtype=torch.float32, device=grads[0].device)
-    with _allocating(stream):
-        work = torch.empty(int(z.lib().zccl_grad_norm_work(len(grads))), dtype=torch.uint8, device=out.device)
-    z._check(z.native().grad_norm(grads, out, work, stream), "zccl_grad_norm")
-    return out
+    return _value(z.native().grad_norm(grads, out, stream), "zccl_grad_norm")
 
 
 def adamw(params, grads, exp_avg, exp_avg_sq, exp_avg_scale=None, exp_avg_sq_scale=None, *, step, lr, betas=(0.9, 0.999), eps=1e-8,

@@ -208,9 +208,12 @@ def test_zeros_and_the_smallest_numbers(optim):
 
 
 def test_rounding_is_unbiased(optim):
-    """The mean over 400 seeds is the value, within five standard deviations of a rounding between two neighbours (half a step at most)."""
+    """The mean over 400 seeds is the value, within five standard deviations of a rounding between two neighbours (half a step at most); roots
+    below the block's smallest element are that element, never 0."""
     n, seeds = 256, 400
-    g = torch.randn(n, device="cuda") * torch.exp2(torch.randint(-6, 1, (n,), device="cuda").float())
+    gen = torch.Generator().manual_seed(0)
+    g = (torch.randn(n, generator=gen) * torch.exp2(torch.randint(-6, 1, (n,), generator=gen).float())).cuda()
+    g[3], g[100] = 1e-12, -1e-7
     total_m, total_r = np.zeros(n), np.zeros(n)
     for seed in range(seeds):
         s = {"p": [torch.zeros(n, device="cuda")], "g": [g], "m": [torch.zeros(n, device="cuda").to(torch.float8_e4m3fn)], "v": [torch.zeros(n, device="cuda").to(torch.float8_e4m3fn)],
@@ -221,7 +224,9 @@ def test_rounding_is_unbiased(optim):
         total_r += np.sqrt(v)
     x = wide(g)
     for total, want in ((total_m, 0.1 * x), (total_r, np.sqrt(0.001) * np.abs(x))):
-        _, _, grid = ref.encode8(want, np.zeros(n), False)
+        _, scale, grid = ref.encode8(want, np.zeros(n), False)
+        if total is total_r:
+            want = np.maximum(want, np.repeat(np.ldexp(2.0 ** -9, scale - 127), 32))
         assert (np.abs(total / seeds - want) <= 5 * 0.5 * grid / np.sqrt(seeds) + 2.0 ** -16 * grid).all()
 
 
