@@ -18,6 +18,8 @@ constexpr int kRowBytes = kDepth / 2;         // an instruction takes 64 element
 constexpr int kProductThreads = 192;          // one warp loads, one issues, four read the sums out
 constexpr uint32_t kWaitLimit = 1u << 22;     // polls of a barrier before giving up
 constexpr uint32_t kStuck = 1u;               // status: a wait ran out
+constexpr int kOutBytes = 64;                 // of a row of the output on its way through shared memory, and their pitch there
+constexpr int kOutPitch = kOutBytes + 16;
 
 __device__ uint32_t g_product_status;
 
@@ -69,6 +71,60 @@ __device__ __forceinline__ void tile_of(const Product& k, uint32_t t, uint32_t b
     row_tile = band * band_tiles + (in - col_tile * high);
 }
 
+// 64 bytes of each of the warp's 32 rows, from registers through shared memory: rows leave as whole sectors, or where they do not begin on 16 bytes as runs
+// of neighbouring elements.  T is the type of the output, `v` has 64 / sizeof(T) columns of the lane's row from c on.
+template <class T>
+__device__ __forceinline__ void store_rows(const Product& k, unsigned char* out, uint32_t r, uint32_t c, const uint32_t* v)
+{
+    constexpr int kPer = 16 / sizeof(T), kWidth = kOutBytes / sizeof(T);
+    const uint32_t lane = threadIdx.x & 31u;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kOutBytes / 16; ++i) {
+        MxPack<T> p;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) p.v[j] = mx_round<T>(__uint_as_float(v[kPer * i + j]));
+        *reinterpret_cast<uint4*>(out + lane * kOutPitch + 16 * i) = *reinterpret_cast<const uint4*>(&p);
+    }
+    __syncwarp();
+    T* const y = (T*)k.y + (size_t)r * k.pitch + c;
+    const uint32_t high = r < k.rows ? min(32u, k.rows - r) : 0u;
+    if (k.wide && c + kWidth <= k.cols) {
+#pragma unroll
+        for (int i = 0; i < kOutBytes / 16; ++i) {
+            const uint32_t row = 8 * i + (lane >> 2), piece = lane & 3u;
+            if (row < high) reinterpret_cast<uint4*>(y + (size_t)row * k.pitch)[piece] = *reinterpret_cast<const uint4*>(out + row * kOutPitch + 16 * piece);
+        }
+    } else {
+        constexpr uint32_t kAtOnce = 32 / kWidth;    // rows of a store
+        const uint32_t at = lane % kWidth;
+        for (uint32_t row = lane / kWidth; row < high; row += kAtOnce)
+            if (c + at < k.cols) y[(size_t)row * k.pitch + at] = *reinterpret_cast<const T*>(out + row * kOutPitch + at * sizeof(T));
+    }
+}
+
+// The sums of one tile out of tensor memory, 128 columns at a time, from its last ones or its first on; `drained` is called once, when the first 128
+// are in registers.
+template <class T, int BN, class F>
+__device__ __forceinline__ void store_tile(const Product& k, unsigned char* out, uint32_t sums, uint32_t r, uint32_t c0, bool from_end, F&& drained)
+{
+    constexpr int kWidth = kOutBytes / sizeof(T);
+#pragma unroll 1
+    for (int i = 0; i < BN / 128; ++i) {
+        const uint32_t c = (from_end ? BN / 128 - 1 - i : i) * 128;
+        uint32_t v[128];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) tcgen05_load32(sums + c + 32 * h, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * h]));
+        tcgen05_wait_loads();
+        if (i == 0) {
+            tcgen05_fence_before();
+            drained();
+        }
+#pragma unroll
+        for (int j = 0; j < 128; j += kWidth) store_rows<T>(k, out, r, c0 + c + j, v + j);
+    }
+}
+
 // ---------------------------------------------------------------- few rows, or few tiles
 
 // A tile of 128 x BN to a cluster, whose CTAs take neighbouring pieces of the contraction.  Their sums are added in the order of the
@@ -81,15 +137,34 @@ struct SplitShape {
     static constexpr int kStages = BN == 128 ? 3 : 4;
     static constexpr int kColAt = kRows * kRowBytes, kRowScaleAt = kColAt + BN * kRowBytes, kColScaleAt = kRowScaleAt + 2 * kMxTileBytes;
     static constexpr int kStage = kColScaleAt + 2 * kMxTileBytes;
-    static constexpr int kScaleColumns = 16;                                     // of tensor memory, for one stage
+    static constexpr int kScaleColumns = 16;                                     // of tensor memory, a set for each stage
     static constexpr int kSumColumns = BN < 32 ? 32 : BN;
-    static constexpr int kColumns = BN <= 32 ? 64 : BN == 64 ? 128 : 256;
-    static constexpr int kSumPitch = kRows + 1;                                  // floats: sums are read along rows and along columns
+    static constexpr int kColumns = BN <= 64 ? 128 : 256;
+    static constexpr int kSumPitch = BN + 4;                                     // floats: rows of sums, read four at a time along rows and along columns
     static constexpr size_t kBytes = (size_t)kStage * kStages + 1024;
-    static_assert(kSumColumns + 2 * kScaleColumns <= kColumns, "tensor memory");
-    static_assert(BN * kSumPitch * 4 <= kStage * kStages, "sums take the stages' place");
+    static_assert(kSumColumns + kStages * kScaleColumns <= kColumns, "tensor memory");
+    static_assert(kRows * kSumPitch * 4 <= kStage * kStages && 4 * 32 * kOutPitch <= kStage * kStages, "sums take the stages' place");
     static_assert((228 * 1024 / kBytes) * kColumns <= 512, "clusters must not wait for each other's tensor memory");
 };
+
+// Four sums, of one row and neighbouring columns, added over the parts in their order.
+__device__ __forceinline__ float4 add_parts(uint32_t at, uint32_t parts)
+{
+    float4 v[8], sum;
+#pragma unroll
+    for (int p = 0; p < 8; ++p)
+        if (p < (int)parts) v[p] = peer_load4(at, p);
+    sum = v[0];
+#pragma unroll
+    for (int p = 1; p < 8; ++p)
+        if (p < (int)parts) {
+            sum.x += v[p].x;
+            sum.y += v[p].y;
+            sum.z += v[p].z;
+            sum.w += v[p].w;
+        }
+    return sum;
+}
 
 template <int BN>
 __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __grid_constant__ CUtensorMap r_map, const __grid_constant__ CUtensorMap c_map, const __grid_constant__ Product k)
@@ -153,7 +228,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
                 if (!wait_for(&full[s], (n / kStages) & 1)) break;
                 tcgen05_fence_after();
                 const uint32_t at = smem_u32(tiles) + s * S::kStage;
-                const uint32_t r_scale = tmem + S::kSumColumns + (n & 1) * S::kScaleColumns, c_scale = r_scale + 8;
+                const uint32_t r_scale = tmem + S::kSumColumns + s * S::kScaleColumns, c_scale = r_scale + 8;
                 for (uint32_t g = 0; g < groups_at(d, k.depth_blocks); ++g) {
                     tcgen05_copy_scales(r_scale + 4 * g, scales_descriptor(at + S::kRowScaleAt + g * kMxTileBytes));
                     tcgen05_copy_scales(c_scale + 4 * g, scales_descriptor(at + S::kColScaleAt + g * kMxTileBytes));
@@ -171,37 +246,51 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
     } else if (wait_for(&done, 0)) {
         tcgen05_fence_after();
         const uint32_t quarter = warp & 3u, row = quarter * 32 + lane;
-        constexpr int kWide = BN < 32 ? BN : 32;
+        if (BN == 128 && parts == 1 && !k.across) {
+            unsigned char* const out = tiles + quarter * 32 * kOutPitch;
+            const uint32_t sums = tmem + (quarter * 32 << 16), r = rt * kRows + quarter * 32;
+            if (k.type == ZCCL_BF16) store_tile<__nv_bfloat16, BN>(k, out, sums, r, c0, false, [] {});
+            else if (k.type == ZCCL_F16) store_tile<__half, BN>(k, out, sums, r, c0, false, [] {});
+            else store_tile<float, BN>(k, out, sums, r, c0, false, [] {});
+        } else {
+            constexpr int kWide = BN < 32 ? BN : 32;
+            float* const to = reinterpret_cast<float*>(tiles) + row * S::kSumPitch;
 #pragma unroll 1
-        for (int c = 0; c < BN; c += kWide) {
-            uint32_t v[32];
-            if (kWide == 32) tcgen05_load32(tmem + (quarter * 32 << 16) + c, v);
-            else tcgen05_load16(tmem + (quarter * 32 << 16) + c, v);
-            tcgen05_wait_loads();
+            for (int c = 0; c < BN; c += kWide) {
+                uint32_t v[32];
+                if (kWide == 32) tcgen05_load32(tmem + (quarter * 32 << 16) + c, v);
+                else tcgen05_load16(tmem + (quarter * 32 << 16) + c, v);
+                tcgen05_wait_loads();
 #pragma unroll
-            for (int j = 0; j < kWide; ++j) reinterpret_cast<float*>(tiles)[(c + j) * S::kSumPitch + row] = __uint_as_float(v[j]);
+                for (int j = 0; j < kWide; j += 4) *reinterpret_cast<uint4*>(to + c + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            }
         }
         tcgen05_fence_before();
     }
     __syncwarp();
     cluster_sync();
-    if (warp >= 2) {
-        const uint32_t sums = smem_u32(tiles), r0 = rt * kRows;
+    if (warp >= 2 && !(BN == 128 && parts == 1 && !k.across)) {
+        const uint32_t sums = smem_u32(tiles), r0 = rt * kRows, thread = threadIdx.x - 64;
         if (k.across) {
-            const uint32_t row = threadIdx.x - 64;
-            for (uint32_t c = part; c < (uint32_t)BN && c0 + c < k.cols; c += parts) {
-                float sum = 0.0f;
-                for (uint32_t p = 0; p < parts; ++p) sum += peer_load(sums + (c * S::kSumPitch + row) * 4, p);
-                if (r0 + row < k.rows) store_one(k, (size_t)(c0 + c) * k.pitch + r0 + row, sum);
+            for (uint32_t c = part * 4; c < (uint32_t)BN && c0 + c < k.cols; c += parts * 4) {
+                const float4 s = add_parts(sums + (thread * S::kSumPitch + c) * 4, parts);
+                const float four[4] = {s.x, s.y, s.z, s.w};
+                if (r0 + thread < k.rows)
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i)
+                        if (c0 + c + i < k.cols) store_one(k, (size_t)(c0 + c + i) * k.pitch + r0 + thread, four[i]);
             }
         } else {
-            for (uint32_t row = part * 4 + warp - 2; row < kRows && r0 + row < k.rows; row += 4 * parts)
-#pragma unroll 4
-                for (uint32_t c = lane; c < (uint32_t)BN; c += 32) {
-                    float sum = 0.0f;
-                    for (uint32_t p = 0; p < parts; ++p) sum += peer_load(sums + (c * S::kSumPitch + row) * 4, p);
-                    if (c0 + c < k.cols) store_one(k, (size_t)(r0 + row) * k.pitch + c0 + c, sum);
-                }
+            constexpr uint32_t kQuads = BN / 4, kAtOnce = 128 / kQuads;      // rows that the four warps take at a time
+            const uint32_t c = thread % kQuads * 4;
+            for (uint32_t row = part * kAtOnce + thread / kQuads; row < kRows && r0 + row < k.rows; row += parts * kAtOnce) {
+                const float4 s = add_parts(sums + (row * S::kSumPitch + c) * 4, parts);
+                const float four[4] = {s.x, s.y, s.z, s.w};
+                const size_t to = (size_t)(r0 + row) * k.pitch + c0 + c;
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i)
+                    if (c0 + c + i < k.cols) store_one(k, to + i, four[i]);
+            }
         }
     }
     __syncwarp();
@@ -214,7 +303,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
 // A pair of CTAs (the two of a cluster) works on a tile of 256 x BN: the first issues instructions that use both tensor cores, each CTA brings and
 // keeps its 128 rows of one operand and half of the other, so an SM reads 128 + BN / 2 rows for 128 x BN sums.  What bounds it is the
 // way from L2 to shared memory: with tiles of 128 x 192 to a single CTA the large product took 157 us (4096 x 8192 x 8192), 12 TB/s.
-// Sums of 256 columns do not fit tensor memory twice next to the scales, so the second set begins 24 columns inside the first; whoever
+// Sums of 256 columns do not fit tensor memory twice next to the scales, so the second set begins 120 columns before the first's end; whoever
 // reads sums out begins with the columns that both have, and says when these are free.
 template <int BN>
 struct PairShape {
@@ -223,70 +312,15 @@ struct PairShape {
     static constexpr int kColAt = kRows * kRowBytes, kRowScaleAt = kColAt + BN / 2 * kRowBytes, kColScaleAt = kRowScaleAt + 2 * kMxTileBytes;
     static constexpr int kStage = kColScaleAt + 2 * kMxTileBytes * kBands;
     static constexpr bool kOverlap = BN == 256;
-    static constexpr int kScaleColumns = 8 + 8 * kBands;                         // for one stage; two sets of them
-    static constexpr int kShared = kOverlap ? 2 * kScaleColumns : 0;             // columns that both sets of sums have
+    static constexpr int kScaleColumns = 8 + 8 * kBands, kScaleSets = kStages;   // of tensor memory, a set for each stage
+    static constexpr int kShared = kOverlap ? kScaleSets * kScaleColumns : 0;    // columns that both sets of sums have
     static constexpr int kSecond = BN - kShared;                                 // where the second set of sums begins
     static constexpr int kScaleAt = kSecond + BN;
     static constexpr int kColumns = 512;
-    static constexpr int kOutPitch = 128 + 16;                                   // bytes of a row on its way out
     static constexpr size_t kBytes = (size_t)kStage * kStages + 4 * 32 * kOutPitch + 1024;
-    static_assert(kScaleAt + 2 * kScaleColumns <= kColumns, "tensor memory");
+    static_assert(kScaleAt + kScaleSets * kScaleColumns <= kColumns && kShared <= 128, "tensor memory");
     static_assert(kBytes <= 227 * 1024 && kBytes > 114 * 1024, "one CTA to an SM");
 };
-
-// 128 bytes of each of the warp's 32 rows, from registers through shared memory: rows leave as whole lines, or where they do not begin on 16 bytes as runs
-// of neighbouring elements.  T is the type of the output, `v` has 128 / sizeof(T) columns of the lane's row from c on.
-template <class T>
-__device__ __forceinline__ void store_rows(const Product& k, unsigned char* out, uint32_t r, uint32_t c, const float (&v)[128 / sizeof(T)])
-{
-    constexpr int kPitch = 128 + 16, kPer = 16 / sizeof(T), kWidth = 128 / sizeof(T);
-    const uint32_t lane = threadIdx.x & 31u;
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        MxPack<T> p;
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) p.v[j] = mx_round<T>(v[kPer * i + j]);
-        *reinterpret_cast<uint4*>(out + lane * kPitch + 16 * i) = *reinterpret_cast<const uint4*>(&p);
-    }
-    __syncwarp();
-    T* const y = (T*)k.y + (size_t)r * k.pitch + c;
-    const uint32_t high = r < k.rows ? min(32u, k.rows - r) : 0u;
-    if (k.wide && c + kWidth <= k.cols) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t row = 4 * i + (lane >> 3), piece = lane & 7u;
-            if (row < high) reinterpret_cast<uint4*>(y + (size_t)row * k.pitch)[piece] = *reinterpret_cast<const uint4*>(out + row * kPitch + 16 * piece);
-        }
-    } else {
-        for (uint32_t row = 0; row < high; ++row)
-#pragma unroll
-            for (int i = 0; i < kWidth / 32; ++i) {
-                const uint32_t at = lane + 32 * i;
-                if (c + at < k.cols) y[(size_t)row * k.pitch + at] = *reinterpret_cast<const T*>(out + row * kPitch + at * sizeof(T));
-            }
-    }
-}
-
-// The sums of one tile out of tensor memory; `drained` is called once, when the columns that the next tile's sums begin in are free.
-template <class T, int BN, class F>
-__device__ __forceinline__ void store_tile(const Product& k, unsigned char* out, uint32_t sums, uint32_t r, uint32_t c0, bool from_end, F&& drained)
-{
-    constexpr int kWidth = 128 / sizeof(T), kPieces = BN / kWidth;
-#pragma unroll 1
-    for (int i = 0; i < kPieces; ++i) {
-        const uint32_t c = (uint32_t)(from_end ? kPieces - 1 - i : i) * kWidth;
-        float v[kWidth];
-#pragma unroll
-        for (int h = 0; h < kWidth / 32; ++h) tcgen05_load32(sums + c + 32 * h, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * h]));
-        tcgen05_wait_loads();
-        if (i == (PairShape<BN>::kOverlap ? (PairShape<BN>::kShared - 1) / kWidth : kPieces - 1)) {
-            tcgen05_fence_before();
-            drained();
-        }
-        store_rows<T>(k, out, r, c0 + c, v);
-    }
-}
 
 template <int BN>
 __global__ void __launch_bounds__(kProductThreads, 1) mx4_pair_kernel(const __grid_constant__ CUtensorMap r_map, const __grid_constant__ CUtensorMap c_map, const __grid_constant__ CUtensorMap r_scale_map,
@@ -339,7 +373,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_pair_kernel(const __gr
                 const int row_band = (int)(rt * 2 + rank), c0 = (int)(ct * BN + rank * (BN / 2));
                 for (uint32_t d = 0; d < depth_tiles; ++d, ++n) {
                     const uint32_t s = n % kStages;
-                    if (n >= kStages && !(ok = wait_for_cluster(&empty[s], (n / kStages - 1) & 1))) break;
+                    if (n >= kStages && !(ok = wait_for(&empty[s], (n / kStages - 1) & 1))) break;
                     unsigned char* const at = tiles + s * S::kStage;
                     const uint32_t bar = address_at(&full[s], 0);
                     if (rank == 0) mbar_expect_tx(&full[s], kBoth);
@@ -355,7 +389,27 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_pair_kernel(const __gr
         }
     } else if (warp == 1) {
         if (rank == 0 && elect_one()) {
-            uint32_t n = 0, i = 0;
+            // What bounds a large product is how fast this thread issues: a stage's instructions run for 512 cycles, and with one wait more to a stage (or the
+            // next stage's scales in front of this one's instructions) 4096 x 8192 x 8192 took 20 to 30 us longer.
+            const uint32_t base = smem_u32(tiles);
+            const auto issue = [&](uint32_t s, uint32_t sums, bool add, uint32_t groups, uint32_t steps) {
+                const uint32_t at = base + s * S::kStage, r_scale = tmem + S::kScaleAt + s * S::kScaleColumns, c_scale = r_scale + 8;
+                const unsigned long long r_codes = operand_descriptor(at), c_codes = operand_descriptor(at + S::kColAt), r_in = scales_descriptor(at + S::kRowScaleAt),
+                                         c_in = scales_descriptor(at + S::kColScaleAt);
+#pragma unroll
+                for (uint32_t g = 0; g < 2; ++g)
+                    if (g < groups) {
+                        tcgen05_copy_scales_pair(r_scale + 4 * g, r_in + g * (kMxTileBytes >> 4));
+#pragma unroll
+                        for (uint32_t b = 0; b < S::kBands; ++b) tcgen05_copy_scales_pair(c_scale + 4 * (g * S::kBands + b), c_in + (b * 2 + g) * (kMxTileBytes >> 4));
+                    }
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j)
+                    if (j < steps)
+                        tcgen05_mma_mx4_pair(sums, r_codes + 2 * j, c_codes + 2 * j, mx4_instruction(2 * kRows, BN, (j & 1) * 2), r_scale + 4 * (j / 2),
+                                             c_scale + 4 * S::kBands * (j / 2), add || j > 0);
+            };
+            uint32_t s = 0, parity = 0, i = 0;
             bool ok = true;
             for (uint32_t t = first; t < total && ok; t += stride, ++i) {
                 const uint32_t sums = tmem + (i & 1) * S::kSecond;
@@ -363,39 +417,31 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_pair_kernel(const __gr
                     if (!(ok = S::kOverlap ? wait_for_cluster(&free_[0], (i - 1) & 1) : wait_for_cluster(&free_[i & 1], (i / 2 - 1) & 1))) break;
                     tcgen05_fence_after();
                 }
-                for (uint32_t d = 0; d < depth_tiles; ++d, ++n) {
-                    const uint32_t s = n % kStages, parity = (n / kStages) & 1;
-                    if (!(ok = wait_for_cluster(&full[s], parity))) break;
+                for (uint32_t d = 0; d < depth_tiles; ++d) {
+                    if (!(ok = wait_for(&full[s], parity))) break;
                     tcgen05_fence_after();
-                    const uint32_t at = smem_u32(tiles) + s * S::kStage;
-                    const uint32_t r_scale = tmem + S::kScaleAt + (n & 1) * S::kScaleColumns, c_scale = r_scale + 8;
-                    for (uint32_t g = 0; g < groups_at(d, k.depth_blocks); ++g) {
-                        tcgen05_copy_scales_pair(r_scale + 4 * g, scales_descriptor(at + S::kRowScaleAt + g * kMxTileBytes));
-#pragma unroll
-                        for (int b = 0; b < S::kBands; ++b)
-                            tcgen05_copy_scales_pair(c_scale + 4 * (g * S::kBands + b), scales_descriptor(at + S::kColScaleAt + (b * 2 + g) * kMxTileBytes));
-                    }
-                    const unsigned long long r_codes = operand_descriptor(at), c_codes = operand_descriptor(at + S::kColAt);
-                    const uint32_t steps = steps_at(d, k.depth_blocks);
-                    for (uint32_t j = 0; j < steps; ++j)
-                        tcgen05_mma_mx4_pair(sums, r_codes + 2 * j, c_codes + 2 * j, mx4_instruction(2 * kRows, BN, (j & 1) * 2), r_scale + 4 * (j / 2),
-                                             c_scale + 4 * S::kBands * (j / 2), d > 0 || j > 0);
+                    if (d + 1 < depth_tiles) issue(s, sums, d > 0, 2, 4);
+                    else issue(s, sums, d > 0, groups_at(d, k.depth_blocks), steps_at(d, k.depth_blocks));
                     tcgen05_commit_pair(&empty[s]);
+                    if (++s == kStages) {
+                        s = 0;
+                        parity ^= 1;
+                    }
                 }
                 tcgen05_commit_pair(&done[i & 1]);
             }
             tcgen05_commit_pair(&drained);
-            wait_for_cluster(&drained, 0);
+            wait_for(&drained, 0);
         }
     } else {
         const uint32_t quarter = warp & 3u;
-        unsigned char* const out = tiles + S::kStage * kStages + quarter * 32 * S::kOutPitch;
+        unsigned char* const out = tiles + S::kStage * kStages + quarter * 32 * kOutPitch;
         uint32_t i = 0;
         for (uint32_t t = first; t < total; t += stride, ++i) {
             uint32_t rt, ct;
             tile_of(k, t, kBand, rt, ct);
             const uint32_t b = i & 1, sums = tmem + b * S::kSecond + (quarter * 32 << 16), r = (rt * 2 + rank) * kRows + quarter * 32;
-            if (!wait_for_cluster(&done[b], (i / 2) & 1)) break;
+            if (!wait_for(&done[b], (i / 2) & 1)) break;
             tcgen05_fence_after();
             const auto free_sums = [&] {
                 __syncwarp();
@@ -577,7 +623,7 @@ int zccl_mx4_matmul(const void* a_codes, const void* a_scales, size_t m, const v
     }
     // whichever is through in less: a round of tiles half as wide takes a little more than half as long
     const size_t pairs = (size_t)dev->pairs, rounds_256 = up(up(sides.rows, 256) * up(sides.cols, 256), pairs), rounds_128 = up(up(sides.rows, 256) * up(sides.cols, 128), pairs);
-    if (rounds_256 * 16 <= rounds_128 * 9) return launch_pair<256>(sides, p, dev->pairs, st);
+    if (rounds_256 <= rounds_128) return launch_pair<256>(sides, p, dev->pairs, st);
     return launch_pair<128>(sides, p, dev->pairs, st);
 }
 

@@ -159,11 +159,12 @@ __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// A word of the shared memory of the cluster's CTA `rank`, at the address `at` of this one's.
-__device__ __forceinline__ float peer_load(uint32_t at, uint32_t rank)
+// Sixteen bytes of the shared memory of the cluster's CTA `rank`, at the address `at` of this one's.
+__device__ __forceinline__ float4 peer_load4(uint32_t at, uint32_t rank)
 {
-    float v;
-    asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}" : "=f"(v) : "r"(at), "r"(rank) : "memory");
+    float4 v;
+    asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n\t}"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at), "r"(rank) : "memory");
     return v;
 }
 
