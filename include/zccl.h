@@ -441,6 +441,13 @@ int zccl_mx4_dequantize(const void* codes, const void* scales, size_t rows, size
 int zccl_mx4_matmul(const void* a_codes, const void* a_scales, size_t m, const void* b_codes, const void* b_scales, size_t n, size_t k,
                     void* y, int type, size_t pitch, void* stream);
 int zccl_mx4_status(void* stream);
+/*
+ * A layer with weights in this form, y [m x n] <- Q(x) W^T in x's type: zccl_mx4_quantize of x [m x k, `x_pitch`] along its rows into x_codes and
+ * x_scales (room for the form of an m x k matrix; for calls that may run at the same time, each its own), then zccl_mx4_matmul, which for few rows begins
+ * to bring the weights while x is still quantised.
+ */
+int zccl_mx4_linear(const void* x, int type, size_t m, size_t k, size_t x_pitch, const void* w_codes, const void* w_scales, size_t n,
+                    void* x_codes, void* x_scales, void* y, size_t pitch, void* stream);
 
 /*
  * What a data-parallel program does with the gradient that the ring has reduced: its norm over all tensors, and the AdamW

@@ -54,7 +54,7 @@ def build_module(force: bool = False) -> Path:
         ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
          f"-I{sysconfig.get_paths()['include']}", f"-I{root / 'include'}", f"-I{root / 'include/torch/csrc/api/include'}", f"-I{cuda / 'include'}",
          "-o", str(tmp), str(MODULE_SOURCE), f"-L{PKG}", "-l:libzccl.so", "-Wl,-rpath,$ORIGIN", f"-L{root / 'lib'}",
-         "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+         "-ltorch_python", "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"])
     os.replace(tmp, MODULE)
     return MODULE
 

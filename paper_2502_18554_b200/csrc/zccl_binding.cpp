@@ -4,7 +4,7 @@
 // (3.3 us of it the look-up of the current stream), here it takes 0.4 us.  The calls themselves are the C boundary's.
 #include <Python.h>
 
-#include <ATen/ops/empty.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
@@ -331,14 +331,15 @@ PyObject* status_on(const at::Tensor& t, F&& f)
 // ---- microscaled 4-bit floating point.  Outputs are allocated here, on the stream that the call runs on: through Python the small
 // allocations of a call took longer than its kernels.
 
-// The device and stream of a call, current for its duration.
+// The device and stream of a call, current for its duration where they are not already.
 struct Place {
     c10::cuda::OptionalCUDAStreamGuard guard;
     void* st = nullptr;
     bool take(PyObject* stream, const at::Tensor& t)
     {
         if (!stream_on(stream, t, &st)) return false;
-        guard.reset_stream(c10::cuda::getStreamFromExternal((cudaStream_t)st, t.device().index()));
+        if (stream != Py_None || c10::cuda::current_device() != t.device().index())
+            guard.reset_stream(c10::cuda::getStreamFromExternal((cudaStream_t)st, t.device().index()));
         return true;
     }
 };
@@ -354,7 +355,8 @@ PyObject* guarded(F&& f)
     }
 }
 
-at::Tensor new_bytes(size_t n, const at::Tensor& like) { return at::empty({(int64_t)n}, like.options().dtype(at::kByte)); }
+at::Tensor new_bytes(size_t n, const at::Tensor& like) { return at::detail::empty_cuda({(int64_t)n}, at::kByte, like.device(), c10::nullopt); }
+at::Tensor new_matrix(size_t rows, size_t cols, c10::ScalarType dt, const at::Tensor& like) { return at::detail::empty_cuda({(int64_t)rows, (int64_t)cols}, dt, like.device(), c10::nullopt); }
 struct Form {
     at::Tensor codes, scales;
 };
@@ -445,7 +447,7 @@ PyObject* mx4_dequantize(PyObject*, Args a, Py_ssize_t na)
     return guarded([&]() -> PyObject* {
         Place place;
         if (!place.take(a[6], *codes)) return nullptr;
-        const at::Tensor out = given ? *y.t : at::empty({(int64_t)rows, (int64_t)cols}, codes->options().dtype(dt));
+        const at::Tensor out = given ? *y.t : new_matrix(rows, cols, dt, *codes);
         return wrapped(zccl_mx4_dequantize(f.codes.data_ptr(), f.scales.data_ptr(), rows, cols, out.data_ptr(), type_of(out), given ? y.pitch : cols, place.st), out);
     });
 }
@@ -468,7 +470,7 @@ PyObject* mx4_matmul(PyObject*, Args a, Py_ssize_t na)
     return guarded([&]() -> PyObject* {
         Place place;
         if (!place.take(a[9], *codes)) return nullptr;
-        const at::Tensor out = given ? *y.t : at::empty({(int64_t)m, (int64_t)n}, codes->options().dtype(dt));
+        const at::Tensor out = given ? *y.t : new_matrix(m, n, dt, *codes);
         return wrapped(zccl_mx4_matmul(l.codes.data_ptr(), l.scales.data_ptr(), m, r.codes.data_ptr(), r.scales.data_ptr(), n, k, out.data_ptr(), type_of(out), given ? y.pitch : n, place.st), out);
     });
 }
@@ -493,13 +495,14 @@ PyObject* mx4_linear(PyObject*, Args a, Py_ssize_t na)
         Place place;
         if (!place.take(Py_None, *x.t)) return nullptr;
         const Form f = new_form(x.rows, x.cols, *x.t);
-        const at::Tensor y = at::empty({(int64_t)x.rows, (int64_t)n}, x.t->options());
-        int rc = x.quantize(false, f, place.st);
-        if (rc == ZCCL_OK && na == 2) {
+        const at::Tensor y = new_matrix(x.rows, n, x.t->scalar_type(), *x.t);
+        int rc = ZCCL_OK;
+        if (na == 2) {
             held = new_form(n, x.cols, *x.t);
             rc = w.quantize(false, held, place.st);
         }
-        if (rc == ZCCL_OK) rc = multiply(f, x.rows, held, n, x.cols, y, place.st);
+        if (rc == ZCCL_OK)
+            rc = zccl_mx4_linear(x.t->data_ptr(), x.type, x.rows, x.cols, x.pitch, held.codes.data_ptr(), held.scales.data_ptr(), n, f.codes.data_ptr(), f.scales.data_ptr(), y.data_ptr(), n, place.st);
         return wrapped(rc, y);
     });
 }
@@ -521,14 +524,14 @@ PyObject* mx4_linear_backward(PyObject*, Args a, Py_ssize_t na)
         int rc = ZCCL_OK;
         if (want_x) {
             const Form l = new_form(m, n, *x.t), r = new_form(k, n, *x.t);
-            dx = at::empty({(int64_t)m, (int64_t)k}, x.t->options());
+            dx = new_matrix(m, k, x.t->scalar_type(), *x.t);
             rc = dy.quantize(false, l, place.st);
             if (rc == ZCCL_OK) rc = w.quantize(true, r, place.st);
             if (rc == ZCCL_OK) rc = multiply(l, m, r, k, n, dx, place.st);
         }
         if (want_w && rc == ZCCL_OK) {
             const Form l = new_form(n, m, *x.t), r = new_form(k, m, *x.t);
-            dw = at::empty({(int64_t)n, (int64_t)k}, w.t->options());
+            dw = new_matrix(n, k, w.t->scalar_type(), *x.t);
             rc = dy.quantize(true, l, place.st);
             if (rc == ZCCL_OK) rc = x.quantize(true, r, place.st);
             if (rc == ZCCL_OK) rc = multiply(l, n, r, k, m, dw, place.st);
@@ -700,7 +703,7 @@ PyObject* grad_norm(PyObject*, Args a, Py_ssize_t na)
     return guarded([&]() -> PyObject* {
         Place place;
         if (!place.take(a[2], like)) return nullptr;
-        const at::Tensor out = given ? *norm : at::empty({1}, like.options().dtype(c10::kFloat));
+        const at::Tensor out = given ? *norm : at::Tensor(at::detail::empty_cuda({1}, c10::kFloat, like.device(), c10::nullopt));
         const at::Tensor work = new_bytes(zccl_grad_norm_work(count), like);
         return wrapped(zccl_grad_norm(at.data(), n.data(), count, type, (float*)out.data_ptr(), work.data_ptr(), place.st), out);
     });

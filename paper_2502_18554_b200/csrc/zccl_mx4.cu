@@ -74,26 +74,31 @@ __device__ __forceinline__ void load8(const T* __restrict__ row, uint32_t at, ui
 }
 
 // Rows: 16 lanes take STRIP groups of 128 neighbouring elements of a row (a group: four blocks, one word of scales), a lane
-// eight elements of each, so loads are 16 bytes a lane and codes leave as whole lines.  Groups of the rows that fill the last band
-// up, and blocks behind the last, are quantised as zeros: only their scales are written.
-// Bound by memory where it is large; with one group at a time the indexes cost more instructions than the elements (23 to an element, 52.5 us
-// for 8192 x 8192 bf16).
+// eight elements of each, so loads are 16 bytes a lane and codes leave as whole lines.  Blocks behind the last are quantised as zeros. CTAs from
+// `work` on write the scales of the rows that fill the last band up, a word a thread.
+// Bound by memory where it is large (8192 x 8192 bf16: 30.5 us, 5.6 TB/s); with one group at a time the indexes cost more instructions than the elements
+// (23 to an element, 52.5 us).
 template <class T, bool VEC, int STRIP>
 __global__ void __launch_bounds__(kMxThreads) mx_quantize_rows_kernel(const T* __restrict__ x, uint32_t rows, uint32_t cols, size_t pitch,
-                                                                       uint32_t blocks, uint32_t groups, uint32_t strips, uint32_t total, uint32_t step_row,
+                                                                       uint32_t blocks, uint32_t groups, uint32_t strips, uint32_t total, uint32_t work, uint32_t step_row,
                                                                        uint32_t step_strip, uint32_t* __restrict__ codes, unsigned char* __restrict__ scales)
 {
     pdl_enter();
+    if (blockIdx.x >= work) {
+        const uint32_t i = (blockIdx.x - work) * kMxThreads + threadIdx.x, r = rows + i / groups;
+        if ((rows - 1) / kMxBand == r / kMxBand) *reinterpret_cast<uint32_t*>(scales + mx_scale_at(r, i % groups, groups)) = 0u;
+        return;
+    }
     const uint32_t sub = threadIdx.x & 15u;
     uint32_t u = blockIdx.x * (kMxThreads / 16) + (threadIdx.x >> 4);
     uint32_t r = u / strips, strip = u - r * strips;
-    const uint32_t stride = gridDim.x * (kMxThreads / 16);
+    const uint32_t stride = work * (kMxThreads / 16);
     // whole warps go round together: the last round's idle half takes part in the exchanges with zeros
     for (uint32_t first = u & ~1u; first < total; first += stride, u += stride) {
         MxTwo<T> v[STRIP][4];
         const uint32_t g0 = strip * STRIP, at = g0 * kMxGroup + sub * 8;
         const T* const row = x + (size_t)r * pitch;
-        const bool there = u < total && r < rows;
+        const bool there = u < total;
 #pragma unroll
         for (int j = 0; j < STRIP; ++j) {
             const uint32_t here = at + j * kMxGroup;
@@ -124,7 +129,7 @@ __global__ void __launch_bounds__(kMxThreads) mx_quantize_rows_kernel(const T* _
             four |= __shfl_xor_sync(kFull, four, 4);
             four |= __shfl_xor_sync(kFull, four, 8);
             if (there && (at >> 5) + 4 * j < blocks) out[16 * j] = w;
-            if (sub == 0 && u < total && g0 + j < groups) *reinterpret_cast<uint32_t*>(scale + j * kMxTileBytes) = four;
+            if (sub == 0 && there && g0 + j < groups) *reinterpret_cast<uint32_t*>(scale + j * kMxTileBytes) = four;
         }
         r += step_row;
         strip += step_strip;
@@ -283,11 +288,12 @@ bool strips_pay(size_t rows, size_t groups) { return groups >= 4 && rows * group
 template <class T, bool VEC>
 cudaError_t launch_rows(const T* x, size_t rows, size_t cols, size_t pitch, void* codes, void* scales, cudaStream_t st)
 {
-    const size_t blocks = mx_blocks(cols), groups = mx_groups(cols), padded = mx_bands(rows) * kMxBand;
-    const bool four = strips_pay(padded, groups);
-    const Rounds k = rounds_of(padded, groups, four ? 4 : 1);
-    return launch_k(four ? mx_quantize_rows_kernel<T, VEC, 4> : mx_quantize_rows_kernel<T, VEC, 1>, dim3(k.ctas), dim3(kMxThreads), 0, st, x, (uint32_t)rows, (uint32_t)cols,
-                    pitch, (uint32_t)blocks, (uint32_t)groups, k.strips, k.total, k.step_row, k.step_strip, (uint32_t*)codes, (unsigned char*)scales);
+    const size_t blocks = mx_blocks(cols), groups = mx_groups(cols), padding = (mx_bands(rows) * kMxBand - rows) * groups;
+    const bool four = strips_pay(rows, groups);
+    const Rounds k = rounds_of(rows, groups, four ? 4 : 1);
+    const unsigned fill = (unsigned)((padding + kMxThreads - 1) / kMxThreads);
+    return launch_k(four ? mx_quantize_rows_kernel<T, VEC, 4> : mx_quantize_rows_kernel<T, VEC, 1>, dim3(k.ctas + fill), dim3(kMxThreads), 0, st, x, (uint32_t)rows, (uint32_t)cols,
+                    pitch, (uint32_t)blocks, (uint32_t)groups, k.strips, k.total, k.ctas, k.step_row, k.step_strip, (uint32_t*)codes, (unsigned char*)scales);
 }
 
 template <class T>

@@ -31,6 +31,7 @@ struct Product {
     uint32_t depth_blocks;                    // blocks of 32 along the contraction
     uint32_t row_tiles, col_tiles;
     int type;
+    int early;                                // the rows' operand is complete when the kernel starts (see mx4_split_kernel)
     int wide;                                 // every row of y begins on a 16-byte boundary
     int across;                               // 1: y is stored the other way round, its rows along the kernel's columns
 };
@@ -60,6 +61,25 @@ __device__ __forceinline__ void store_one(const Product& k, size_t to, float v)
     if (k.type == ZCCL_BF16) ((__nv_bfloat16*)k.y)[to] = mx_round<__nv_bfloat16>(v);
     else if (k.type == ZCCL_F16) ((__half*)k.y)[to] = mx_round<__half>(v);
     else ((float*)k.y)[to] = v;
+}
+
+// Up to four neighbouring elements of y, `left` of which are inside.
+__device__ __forceinline__ void store_four(const Product& k, size_t to, uint32_t left, const float (&v)[4])
+{
+    if (k.wide && left >= 4) {
+        if (k.type == ZCCL_F32) *reinterpret_cast<float4*>((float*)k.y + to) = make_float4(v[0], v[1], v[2], v[3]);
+        else {
+            ushort4 h;
+            unsigned short* const e = &h.x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i] = k.type == ZCCL_BF16 ? __bfloat16_as_ushort(mx_round<__nv_bfloat16>(v[i])) : __half_as_ushort(mx_round<__half>(v[i]));
+            *reinterpret_cast<ushort4*>((unsigned short*)k.y + to) = h;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if ((uint32_t)i < left) store_one(k, to + i, v[i]);
+    }
 }
 
 // Tile t of the output: `high` tiles of rows share a walk along the columns, so what is in flight reads few rows and columns.
@@ -140,14 +160,15 @@ struct SplitShape {
     static constexpr int kScaleColumns = 16;                                     // of tensor memory, a set for each stage
     static constexpr int kSumColumns = BN < 32 ? 32 : BN;
     static constexpr int kColumns = BN <= 64 ? 128 : 256;
-    static constexpr int kSumPitch = BN + 4;                                     // floats: rows of sums, read four at a time along rows and along columns
+    static constexpr int kSumPitch = BN + 4;                                     // floats to a row of sums; across, sums are kept column by column instead
     static constexpr size_t kBytes = (size_t)kStage * kStages + 1024;
     static_assert(kSumColumns + kStages * kScaleColumns <= kColumns, "tensor memory");
     static_assert(kRows * kSumPitch * 4 <= kStage * kStages && 4 * 32 * kOutPitch <= kStage * kStages, "sums take the stages' place");
     static_assert((228 * 1024 / kBytes) * kColumns <= 512, "clusters must not wait for each other's tensor memory");
 };
 
-// Four sums, of one row and neighbouring columns, added over the parts in their order.
+// Four neighbouring sums, added over the parts in their order.  A warp's 32 lanes read 512 bytes in a row: what lies apart in another SM's memory comes
+// at a fraction of the speed.
 __device__ __forceinline__ float4 add_parts(uint32_t at, uint32_t parts)
 {
     float4 v[8], sum;
@@ -192,7 +213,6 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
     __syncthreads();
     tcgen05_fence_after();
     const uint32_t tmem = tmem_at;
-    pdl_enter();
 
     uint32_t parts;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
@@ -200,22 +220,33 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
     const uint32_t k_begin = (uint32_t)((unsigned long long)depth_tiles * part / parts), k_end = (uint32_t)((unsigned long long)depth_tiles * (part + 1) / parts);
     uint32_t rt, ct;
     tile_of(k, blockIdx.x / parts, 8, rt, ct);
-    const uint32_t c0 = ct * BN;
+    const uint32_t c0 = ct * BN, groups = (k.depth_blocks + 3) / 4;
+    const auto load_rows = [&](uint32_t s, uint32_t d) {
+        unsigned char* const at = tiles + s * S::kStage;
+        const uint32_t scale_bytes = groups_at(d, k.depth_blocks) * kMxTileBytes;
+        mbar_expect_tx(&full[s], (kRows + BN) * kRowBytes + 2 * scale_bytes);
+        tile_load(at, &r_map, (int)(d * kRowBytes), (int)(rt * kRows), &full[s]);
+        bytes_load(at + S::kRowScaleAt, k.r_scales + ((size_t)rt * groups + 2 * d) * kMxTileBytes, scale_bytes, &full[s]);
+    };
+    // The kernel in front may still be at work on the columns' operand, so the rows' is asked for already: with `early` it was complete when that kernel
+    // let this one start, since that one had waited for all before it.
+    const bool loads = warp == 0 && lane == 0;
+    uint32_t asked = 0;
+    if (loads && k.early)
+        for (; asked < (uint32_t)kStages && k_begin + asked < k_end; ++asked) load_rows(asked, k_begin + asked);
+    __syncwarp();
+    pdl_enter();
 
     if (warp == 0) {
-        if (lane == 0) {
-            const uint32_t groups = (k.depth_blocks + 3) / 4;
+        if (loads) {
             uint32_t n = 0;
             for (uint32_t d = k_begin; d < k_end; ++d, ++n) {
                 const uint32_t s = n % kStages;
                 if (n >= kStages && !wait_for(&empty[s], (n / kStages - 1) & 1)) break;
+                if (n >= asked) load_rows(s, d);
                 unsigned char* const at = tiles + s * S::kStage;
-                const uint32_t scale_bytes = groups_at(d, k.depth_blocks) * kMxTileBytes;
-                mbar_expect_tx(&full[s], (kRows + BN) * kRowBytes + 2 * scale_bytes);
-                tile_load(at, &r_map, (int)(d * kRowBytes), (int)(rt * kRows), &full[s]);
                 tile_load(at + S::kColAt, &c_map, (int)(d * kRowBytes), (int)c0, &full[s]);
-                bytes_load(at + S::kRowScaleAt, k.r_scales + ((size_t)rt * groups + 2 * d) * kMxTileBytes, scale_bytes, &full[s]);
-                bytes_load(at + S::kColScaleAt, k.c_scales + ((size_t)(c0 / kMxBand) * groups + 2 * d) * kMxTileBytes, scale_bytes, &full[s]);
+                bytes_load(at + S::kColScaleAt, k.c_scales + ((size_t)(c0 / kMxBand) * groups + 2 * d) * kMxTileBytes, groups_at(d, k.depth_blocks) * kMxTileBytes, &full[s]);
             }
             // what has been asked for lands before the memory is given up, whether it is used or not
             for (uint32_t i = n < kStages ? 0 : n - kStages; i < n; ++i) wait_for(&full[i % kStages], (i / kStages) & 1);
@@ -254,15 +285,21 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
             else store_tile<float, BN>(k, out, sums, r, c0, false, [] {});
         } else {
             constexpr int kWide = BN < 32 ? BN : 32;
-            float* const to = reinterpret_cast<float*>(tiles) + row * S::kSumPitch;
+            float* const to = reinterpret_cast<float*>(tiles) + (k.across ? row : row * S::kSumPitch);
 #pragma unroll 1
             for (int c = 0; c < BN; c += kWide) {
+                if (k.across && c0 + c >= k.cols) break;
                 uint32_t v[32];
                 if (kWide == 32) tcgen05_load32(tmem + (quarter * 32 << 16) + c, v);
                 else tcgen05_load16(tmem + (quarter * 32 << 16) + c, v);
                 tcgen05_wait_loads();
+                if (k.across) {
 #pragma unroll
-                for (int j = 0; j < kWide; j += 4) *reinterpret_cast<uint4*>(to + c + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                    for (int j = 0; j < kWide; ++j) to[(c + j) * kRows] = __uint_as_float(v[j]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kWide; j += 4) *reinterpret_cast<uint4*>(to + c + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                }
             }
         }
         tcgen05_fence_before();
@@ -272,13 +309,10 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
     if (warp >= 2 && !(BN == 128 && parts == 1 && !k.across)) {
         const uint32_t sums = smem_u32(tiles), r0 = rt * kRows, thread = threadIdx.x - 64;
         if (k.across) {
-            for (uint32_t c = part * 4; c < (uint32_t)BN && c0 + c < k.cols; c += parts * 4) {
-                const float4 s = add_parts(sums + (thread * S::kSumPitch + c) * 4, parts);
+            for (uint32_t c = part * 4 + warp - 2; c < (uint32_t)BN && c0 + c < k.cols; c += parts * 4) {
+                const float4 s = add_parts(sums + (c * kRows + lane * 4) * 4, parts);
                 const float four[4] = {s.x, s.y, s.z, s.w};
-                if (r0 + thread < k.rows)
-#pragma unroll
-                    for (uint32_t i = 0; i < 4; ++i)
-                        if (c0 + c + i < k.cols) store_one(k, (size_t)(c0 + c + i) * k.pitch + r0 + thread, four[i]);
+                store_four(k, (size_t)(c0 + c) * k.pitch + r0 + lane * 4, k.rows - min(k.rows, r0 + lane * 4), four);
             }
         } else {
             constexpr uint32_t kQuads = BN / 4, kAtOnce = 128 / kQuads;      // rows that the four warps take at a time
@@ -286,10 +320,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
             for (uint32_t row = part * kAtOnce + thread / kQuads; row < kRows && r0 + row < k.rows; row += parts * kAtOnce) {
                 const float4 s = add_parts(sums + (row * S::kSumPitch + c) * 4, parts);
                 const float four[4] = {s.x, s.y, s.z, s.w};
-                const size_t to = (size_t)(r0 + row) * k.pitch + c0 + c;
-#pragma unroll
-                for (uint32_t i = 0; i < 4; ++i)
-                    if (c0 + c + i < k.cols) store_one(k, to + i, four[i]);
+                store_four(k, (size_t)(r0 + row) * k.pitch + c0 + c, k.cols - min(k.cols, c0 + c), four);
             }
         }
     }
@@ -574,14 +605,8 @@ int launch_pair(const Sides& s, Product k, int pairs, cudaStream_t st)
 
 bool aligned16(const void* p) { return p && ((uintptr_t)p & 15u) == 0; }
 
-}  // namespace
-}  // namespace zccl
-
-using namespace zccl;
-
-extern "C" {
-
-int zccl_mx4_matmul(const void* a_codes, const void* a_scales, size_t m, const void* b_codes, const void* b_scales, size_t n, size_t k, void* y, int type, size_t pitch, void* stream)
+// `weights_ready`: B was complete before the kernel in front on the stream started.
+int multiply(const void* a_codes, const void* a_scales, size_t m, const void* b_codes, const void* b_scales, size_t n, size_t k, void* y, int type, size_t pitch, bool weights_ready, void* stream)
 {
     if (type < ZCCL_F32 || type > ZCCL_F16) return ZCCL_E_ARG;
     const size_t element = type == ZCCL_F32 ? 4 : 2;
@@ -604,6 +629,7 @@ int zccl_mx4_matmul(const void* a_codes, const void* a_scales, size_t m, const v
     p.r_scales = (const unsigned char*)a_scales;
     p.c_scales = (const unsigned char*)b_scales;
     p.across = m < n && m <= 128;
+    p.early = weights_ready && p.across;
     if (p.across) {
         std::swap(sides.r_codes, sides.c_codes);
         std::swap(sides.rows, sides.cols);
@@ -625,6 +651,26 @@ int zccl_mx4_matmul(const void* a_codes, const void* a_scales, size_t m, const v
     const size_t pairs = (size_t)dev->pairs, rounds_256 = up(up(sides.rows, 256) * up(sides.cols, 256), pairs), rounds_128 = up(up(sides.rows, 256) * up(sides.cols, 128), pairs);
     if (rounds_256 <= rounds_128) return launch_pair<256>(sides, p, dev->pairs, st);
     return launch_pair<128>(sides, p, dev->pairs, st);
+}
+
+}  // namespace
+}  // namespace zccl
+
+using namespace zccl;
+
+extern "C" {
+
+int zccl_mx4_matmul(const void* a_codes, const void* a_scales, size_t m, const void* b_codes, const void* b_scales, size_t n, size_t k, void* y, int type, size_t pitch, void* stream)
+{
+    return multiply(a_codes, a_scales, m, b_codes, b_scales, n, k, y, type, pitch, false, stream);
+}
+
+int zccl_mx4_linear(const void* x, int type, size_t m, size_t k, size_t x_pitch, const void* w_codes, const void* w_scales, size_t n, void* x_codes, void* x_scales, void* y, size_t pitch, void* stream)
+{
+    if (m == 0 || n == 0 || k == 0) return multiply(x_codes, x_scales, m, w_codes, w_scales, n, k, y, type, pitch, false, stream);
+    if (!aligned16(w_codes) || !aligned16(w_scales) || pitch < n || !y || (uintptr_t)y % (type == ZCCL_F32 ? 4 : 2)) return ZCCL_E_ARG;
+    const int rc = zccl_mx4_quantize(x, type, m, k, x_pitch, 0, x_codes, x_scales, stream);
+    return rc == ZCCL_OK ? multiply(x_codes, x_scales, m, w_codes, w_scales, n, k, y, type, pitch, true, stream) : rc;
 }
 
 int zccl_mx4_status(void* stream)
