@@ -352,7 +352,7 @@ __device__ __forceinline__ void encode_states(const AdamRates& k, unsigned long 
     vc = pack8<true>(r, second, vs);
 }
 
-// A CTA takes a chunk of `passes` times 2048 elements of one tensor, a thread eight neighbours at a time.  Chunks that are whole, of arrays on
+// A CTA takes a chunk of `passes` times 2048 elements of one tensor, a thread eight neighbours at a time.  Passes that are whole, of arrays on
 // 16-byte boundaries, go the short way, where the next eight are loaded while these are worked on.  States in 32 bits: bound by memory, two CTAs to an SM
 // have enough loads in flight.  In 8 bits: about 50 instructions to an element against 10 bytes, so issue and memory take about as long and warps have
 // to cover each other's waits: four CTAs, though a few registers are spilled for it (128 Mi bf16 parameters: 261 us, with two or three CTAs 335).
@@ -387,7 +387,8 @@ __global__ void __launch_bounds__(kOptThreads, EIGHT ? 4 : 2) adamw_kernel(const
     const uint32_t chunk = call.passes * kPass;
     const unsigned long long begin = (unsigned long long)(blockIdx.x - list.first[t]) * chunk;
     const uint32_t mine = threadIdx.x * kPerThread;
-    if (a.wide && a.n - begin >= chunk) {
+    const int left_all = (int)min((unsigned long long)chunk, a.n - begin), whole = a.wide ? left_all / kPass : 0;   // passes that go the short way
+    if (whole) {
         P* p = (P*)a.p + begin + mine;
         const G* g = (const G*)a.g + begin + mine;
         unsigned char* copy = a.copy ? (unsigned char*)a.copy + 2 * (begin + mine) : nullptr;
@@ -399,14 +400,14 @@ __global__ void __launch_bounds__(kOptThreads, EIGHT ? 4 : 2) adamw_kernel(const
             unsigned char *ms = a.m_scale + (begin + mine) / kMxBlock, *vs = a.v_scale + (begin + mine) / kMxBlock;
             uint2 me = __ldcs(reinterpret_cast<const uint2*>(mc)), ve = __ldcs(reinterpret_cast<const uint2*>(vc));
             uint32_t mu = *ms, vu = *vs;
-            for (uint32_t i = 1; i <= call.passes; ++i) {
+            for (int i = 1; i <= whole; ++i) {
                 float pv[8], gv[8], mv[8], vv[8], rv[8];
                 values_of(pe, pv);
                 values_of(ge, gv);
                 decode8(me, mv);
                 decode8(ve, vv);
                 const float m_unit = call.beta1 * mx_scale(mu), v_unit = call.root_beta2 * mx_scale(vu);
-                if (i < call.passes) {
+                if (i < whole) {
                     pe = load_wide(p + kPass);
                     ge = load_wide(g + kPass);
                     me = __ldcs(reinterpret_cast<const uint2*>(mc + kPass));
@@ -435,14 +436,14 @@ __global__ void __launch_bounds__(kOptThreads, EIGHT ? 4 : 2) adamw_kernel(const
         } else {
             float *m = (float*)a.m + begin + mine, *v = (float*)a.v + begin + mine;
             Eight<float> me = load_wide(m), ve = load_wide(v);
-            for (uint32_t i = 1; i <= call.passes; ++i) {
+            for (int i = 1; i <= whole; ++i) {
                 float pv[8], gv[8], mv[8], vv[8], rv[8];
                 values_of(pe, pv);
                 values_of(ge, gv);
                 values_of(me, mv);
                 values_of(ve, vv);
                 update8<false>(call, k, call.beta1, call.beta2, gv, pv, mv, vv, rv);
-                if (i < call.passes) {
+                if (i < whole) {
                     pe = load_wide(p + kPass);
                     ge = load_wide(g + kPass);
                     me = load_wide((const float*)m + kPass);
@@ -459,13 +460,11 @@ __global__ void __launch_bounds__(kOptThreads, EIGHT ? 4 : 2) adamw_kernel(const
                 p += kPass; g += kPass; m += kPass; v += kPass;
             }
         }
-        return;
     }
-    const int left_all = (int)min((unsigned long long)chunk, a.n - begin);
     P* const p = (P*)a.p + begin;
     const G* const g = (const G*)a.g + begin;
     const bool p_wide = wide(p), g_wide = wide(g), copies = a.copy != nullptr, copy_wide = wide((const __half*)a.copy);
-    for (int at = mine; at - (int)(threadIdx.x & 31) * kPerThread < left_all; at += kPass) {   // whole warps
+    for (int at = whole * kPass + (int)mine; at - (int)(threadIdx.x & 31) * kPerThread < left_all; at += kPass) {   // whole warps
         const int left = left_all - at;
         const bool all = left >= 8;
         float pv[8], gv[8], mv[8], vv[8], rv[8];
@@ -682,9 +681,10 @@ int zccl_adamw(const zccl_adamw_tensor* tensors, size_t count, const zccl_adamw_
     call.norm = k.norm;
     call.max_norm = (float)k.max_norm;
     call.copy_type = k.copy_type;
-    // Small models are spread over the SMs; large ones have chunks of up to eight passes, whose first loads alone are not covered by work.
+    // Small models are spread over the SMs; large ones have chunks of four passes, whose first loads alone are not covered by work (with two of
+    // them 128 Mi parameters with states in 8 bits took 298 us instead of 280, with eight 64 Mi with 32 bits 326 instead of 317: more is left at the end).
     call.passes = 1;
-    while (call.passes < 8 && total / kPass > (size_t)kChunksWanted * call.passes) call.passes *= 2;
+    while (call.passes < 4 && total / kPass > (size_t)kChunksWanted * call.passes) call.passes *= 2;
     return used <= (size_t)kFewTensors ? run_list<kFewTensors>(tensors, count, k, call, (cudaStream_t)stream)
                                        : run_list<kManyTensors>(tensors, count, k, call, (cudaStream_t)stream);
 }

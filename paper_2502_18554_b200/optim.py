@@ -9,6 +9,8 @@ import torch
 from . import zccl as z
 from .mx import _value
 
+BLOCK = 32
+
 
 def grad_norm(grads, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """sqrt(sum of g^2) over all of `grads` (CUDA tensors of one type), as a float32 [1] on their device."""
@@ -26,3 +28,68 @@ def adamw(params, grads, exp_avg, exp_avg_sq, exp_avg_scale=None, exp_avg_sq_sca
     grad_norm) gradients are scaled to `max_norm` at most, and a norm that is not finite leaves everything as it was."""
     z._check(z.native().adamw(params, grads, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale, copies, lr, betas[0], betas[1], eps,
                               weight_decay, step, seed, norm, max_norm, stream), "zccl_adamw")
+
+
+def exchange(ring, grads, eb_mode: int, eb: float) -> list[torch.Tensor]:
+    """The gradients' average over the ranks of `ring` (a `ring.Ring`), compressed on the way: one Allreduce of all of them, as float32, in
+    which every rank ends with the same values (ZCCL_CONSISTENT_OWNER).  Returns tensors of the gradients' shapes, views of one array in which each
+    begins at a multiple of 32 elements; the gaps hold zeros, which count into the range that a relative bound refers to."""
+    at, spans = 0, []
+    for g in grads:
+        spans.append((at, g.numel()))
+        at += -(-g.numel() // BLOCK) * BLOCK
+    flat = torch.zeros(at, dtype=torch.float32, device=ring.codec.device)
+    if spans:
+        torch._foreach_copy_([flat[o:o + n].view(g.shape) for (o, n), g in zip(spans, grads)], list(grads))
+    reduced = torch.empty_like(flat)
+    ring.allreduce(flat, reduced, eb_mode, eb, flags=z.OP_AVG | z.CONSISTENT_OWNER)
+    return [reduced[o:o + n].view(g.shape) for (o, n), g in zip(spans, grads)]
+
+
+class AdamW:
+    """AdamW over the contiguous CUDA tensors `params` (all of one type), with its states in 32 or 8 bits.
+
+    step() takes the gradients from the parameters' `.grad`, or those it is given; `exchange` makes the ranks of a data-parallel job
+    agree on them first.  `copies` receive the new parameters as in adamw()."""
+
+    def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, state_bits: int = 32, copies=None, seed: int = 0):
+        if state_bits not in (32, 8):
+            raise ValueError("state_bits is 32 or 8")
+        self.params, self.copies = list(params), None if copies is None else list(copies)
+        self.lr, self.betas, self.eps, self.weight_decay, self.seed = lr, betas, eps, weight_decay, seed
+        self.steps = 0
+        dtype = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
+        state = lambda: [torch.zeros(p.shape, dtype=dtype, device=p.device) for p in self.params]  # noqa: E731
+        scale = lambda: [torch.zeros(-(-p.numel() // BLOCK), dtype=torch.uint8, device=p.device) for p in self.params]  # noqa: E731
+        self.exp_avg, self.exp_avg_sq = state(), state()
+        self.exp_avg_scale, self.exp_avg_sq_scale = (scale(), scale()) if state_bits == 8 else (None, None)
+
+    def step(self, grads=None, max_norm: float | None = None, ring=None, eb_mode: int = z.EB_REL, eb: float = 1e-3, stream=None) -> torch.Tensor | None:
+        """One step.  `ring`: exchange the gradients over its ranks first, with this error bound (then on the current stream).  `max_norm`: scale them to
+        that norm at most; returns the norm (float32 [1], on the device).  A step whose norm is not finite changes nothing but `steps`."""
+        grads = [p.grad for p in self.params] if grads is None else list(grads)
+        if any(g is None for g in grads):
+            raise ValueError("every parameter needs a gradient")
+        if ring is not None:
+            if stream is not None:
+                raise ValueError("an exchange runs on the current stream")
+            grads = exchange(ring, grads, eb_mode, eb)
+        norm = None if max_norm is None else grad_norm(grads, stream=stream)
+        self.steps += 1
+        adamw(self.params, grads, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale, self.exp_avg_sq_scale, step=self.steps, lr=self.lr, betas=self.betas, eps=self.eps,
+              weight_decay=self.weight_decay, copies=self.copies, norm=norm, max_norm=1.0 if max_norm is None else max_norm, seed=self.seed, stream=stream)
+        return norm
+
+    def state_dict(self) -> dict:
+        """Steps so far and the states (the tensors themselves)."""
+        return {"steps": self.steps, "exp_avg": self.exp_avg, "exp_avg_sq": self.exp_avg_sq, "exp_avg_scale": self.exp_avg_scale, "exp_avg_sq_scale": self.exp_avg_sq_scale}
+
+    def load_state_dict(self, state: dict) -> None:
+        for key in ("exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale"):
+            mine, theirs = getattr(self, key), state[key]
+            if (mine is None) != (theirs is None) or (mine is not None and [(t.shape, t.dtype) for t in mine] != [(t.shape, t.dtype) for t in theirs]):
+                raise ValueError(f"{key} does not fit these parameters and this state_bits")
+        for key in ("exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale"):
+            for m, t in zip(getattr(self, key) or (), state[key] or ()):
+                m.copy_(t)
+        self.steps = state["steps"]

@@ -135,7 +135,7 @@ def test_tensors_that_begin_anywhere(optim, bits, shift):
     check(s, before, HYPER, bits, seed=3)
 
 
-@pytest.mark.parametrize("count", [40, 41, 380, 381, 1000])
+@pytest.mark.parametrize("count", [40, 41, 42, 364, 365, 380, 381, 1000])
 def test_many_tensors(optim, count):
     """The numbers of tensors around which the list's form and the number of launches change."""
     sizes = [(7 * i) % 97 for i in range(count - 1)] + [20_000]
