@@ -15,7 +15,7 @@ namespace {
 constexpr int kRows = 128;                    // rows of a tile: the tensor core's lanes
 constexpr int kDepth = 256;                   // elements along the contraction per stage: 128 bytes of codes, a row of the swizzle
 constexpr int kRowBytes = kDepth / 2;         // an instruction takes 64 elements, 32 bytes of them
-constexpr int kProductThreads = 192;          // one warp loads, one issues, four read the sums out
+constexpr int kProductThreads = 192;          // one warp loads, one issues, four read the sums out (eight in pairs of CTAs)
 constexpr uint32_t kWaitLimit = 1u << 22;     // polls of a barrier before giving up
 constexpr uint32_t kStuck = 1u;               // status: a wait ran out
 constexpr int kOutBytes = 64;                 // of a row of the output on its way through shared memory, and their pitch there
@@ -123,26 +123,26 @@ __device__ __forceinline__ void store_rows(const Product& k, unsigned char* out,
     }
 }
 
-// The sums of one tile out of tensor memory, 128 columns at a time, from its last ones or its first on; `drained` is called once, when the first 128
-// are in registers.
-template <class T, int BN, class F>
-__device__ __forceinline__ void store_tile(const Product& k, unsigned char* out, uint32_t sums, uint32_t r, uint32_t c0, bool from_end, F&& drained)
+// `COLS` columns of the warp's 32 rows out of tensor memory; `drained` is called when they are in registers.
+template <class T, int COLS, class F>
+__device__ __forceinline__ void store_columns(const Product& k, unsigned char* out, uint32_t sums, uint32_t r, uint32_t c, F&& drained)
 {
     constexpr int kWidth = kOutBytes / sizeof(T);
-#pragma unroll 1
-    for (int i = 0; i < BN / 128; ++i) {
-        const uint32_t c = (from_end ? BN / 128 - 1 - i : i) * 128;
-        uint32_t v[128];
+    uint32_t v[COLS];
 #pragma unroll
-        for (int h = 0; h < 4; ++h) tcgen05_load32(sums + c + 32 * h, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * h]));
-        tcgen05_wait_loads();
-        if (i == 0) {
-            tcgen05_fence_before();
-            drained();
-        }
+    for (int h = 0; h < COLS; h += 32) tcgen05_load32(sums + h, *reinterpret_cast<uint32_t(*)[32]>(&v[h]));
+    tcgen05_wait_loads();
+    tcgen05_fence_before();
+    drained();
 #pragma unroll
-        for (int j = 0; j < 128; j += kWidth) store_rows<T>(k, out, r, c0 + c + j, v + j);
-    }
+    for (int j = 0; j < COLS; j += kWidth) store_rows<T>(k, out, r, c + j, v + j);
+}
+template <int COLS, class F>
+__device__ __forceinline__ void store_columns_any(const Product& k, unsigned char* out, uint32_t sums, uint32_t r, uint32_t c, F&& drained)
+{
+    if (k.type == ZCCL_BF16) store_columns<__nv_bfloat16, COLS>(k, out, sums, r, c, drained);
+    else if (k.type == ZCCL_F16) store_columns<__half, COLS>(k, out, sums, r, c, drained);
+    else store_columns<float, COLS>(k, out, sums, r, c, drained);
 }
 
 // ---------------------------------------------------------------- few rows, or few tiles
@@ -280,9 +280,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
         if (BN == 128 && parts == 1 && !k.across) {
             unsigned char* const out = tiles + quarter * 32 * kOutPitch;
             const uint32_t sums = tmem + (quarter * 32 << 16), r = rt * kRows + quarter * 32;
-            if (k.type == ZCCL_BF16) store_tile<__nv_bfloat16, BN>(k, out, sums, r, c0, false, [] {});
-            else if (k.type == ZCCL_F16) store_tile<__half, BN>(k, out, sums, r, c0, false, [] {});
-            else store_tile<float, BN>(k, out, sums, r, c0, false, [] {});
+            store_columns_any<128>(k, out, sums, r, c0, [] {});
         } else {
             constexpr int kWide = BN < 32 ? BN : 32;
             float* const to = reinterpret_cast<float*>(tiles) + (k.across ? row : row * S::kSumPitch);
@@ -334,27 +332,26 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
 // A pair of CTAs (the two of a cluster) works on a tile of 256 x BN: the first issues instructions that use both tensor cores, each CTA brings and
 // keeps its 128 rows of one operand and half of the other, so an SM reads 128 + BN / 2 rows for 128 x BN sums.  What bounds it is the
 // way from L2 to shared memory: with tiles of 128 x 192 to a single CTA the large product took 157 us (4096 x 8192 x 8192), 12 TB/s.
-// Sums of 256 columns do not fit tensor memory twice next to the scales, so the second set begins 120 columns before the first's end; whoever
-// reads sums out begins with the columns that both have, and says when these are free.
+// Eight warps read a tile's sums out, each half of the columns of a quarter of the rows, all into registers at once: sums of 256 columns do not fit tensor
+// memory twice next to the scales, so the next tile's instructions wait for that (of 128 columns there are two sets).
+constexpr int kPairWarps = 8, kPairThreads = 64 + 32 * kPairWarps;
 template <int BN>
 struct PairShape {
     static constexpr int kStages = BN == 256 ? 5 : 7;
     static constexpr int kBands = BN / kMxBand;                                  // tiles of scales that a tile's columns lie in
     static constexpr int kColAt = kRows * kRowBytes, kRowScaleAt = kColAt + BN / 2 * kRowBytes, kColScaleAt = kRowScaleAt + 2 * kMxTileBytes;
     static constexpr int kStage = kColScaleAt + 2 * kMxTileBytes * kBands;
-    static constexpr bool kOverlap = BN == 256;
-    static constexpr int kScaleColumns = 8 + 8 * kBands, kScaleSets = kStages;   // of tensor memory, a set for each stage
-    static constexpr int kShared = kOverlap ? kScaleSets * kScaleColumns : 0;    // columns that both sets of sums have
-    static constexpr int kSecond = BN - kShared;                                 // where the second set of sums begins
-    static constexpr int kScaleAt = kSecond + BN;
+    static constexpr int kScaleColumns = 8 + 8 * kBands;                         // of tensor memory, a set for each stage
+    static constexpr int kSums = BN == 256 ? 1 : 2;
+    static constexpr int kScaleAt = kSums * BN;
     static constexpr int kColumns = 512;
-    static constexpr size_t kBytes = (size_t)kStage * kStages + 4 * 32 * kOutPitch + 1024;
-    static_assert(kScaleAt + kScaleSets * kScaleColumns <= kColumns && kShared <= 128, "tensor memory");
+    static constexpr size_t kBytes = (size_t)kStage * kStages + kPairWarps * 32 * kOutPitch + 1024;
+    static_assert(kScaleAt + kStages * kScaleColumns <= kColumns, "tensor memory");
     static_assert(kBytes <= 227 * 1024 && kBytes > 114 * 1024, "one CTA to an SM");
 };
 
 template <int BN>
-__global__ void __launch_bounds__(kProductThreads, 1) mx4_pair_kernel(const __grid_constant__ CUtensorMap r_map, const __grid_constant__ CUtensorMap c_map, const __grid_constant__ CUtensorMap r_scale_map,
+__global__ void __launch_bounds__(kPairThreads, 1) mx4_pair_kernel(const __grid_constant__ CUtensorMap r_map, const __grid_constant__ CUtensorMap c_map, const __grid_constant__ CUtensorMap r_scale_map,
                                                                       const __grid_constant__ CUtensorMap c_scale_map, const __grid_constant__ Product k)
 {
     using S = PairShape<BN>;
@@ -376,7 +373,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_pair_kernel(const __gr
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&done[i], 1);
-            mbar_init(&free_[i], 8);
+            mbar_init(&free_[i], 2 * kPairWarps);
         }
         mbar_init(&drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -443,9 +440,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_pair_kernel(const __gr
             uint32_t s = 0, parity = 0, i = 0;
             bool ok = true;
             for (uint32_t t = first; t < total && ok; t += stride, ++i) {
-                const uint32_t sums = tmem + (i & 1) * S::kSecond;
-                if (S::kOverlap ? i >= 1 : i >= 2) {
-                    if (!(ok = S::kOverlap ? wait_for_cluster(&free_[0], (i - 1) & 1) : wait_for_cluster(&free_[i & 1], (i / 2 - 1) & 1))) break;
+                const uint32_t b = i % S::kSums, sums = tmem + b * BN;
+                if (i >= S::kSums) {
+                    if (!(ok = wait_for_cluster(&free_[b], (i / S::kSums - 1) & 1))) break;
                     tcgen05_fence_after();
                 }
                 for (uint32_t d = 0; d < depth_tiles; ++d) {
@@ -459,28 +456,25 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_pair_kernel(const __gr
                         parity ^= 1;
                     }
                 }
-                tcgen05_commit_pair(&done[i & 1]);
+                tcgen05_commit_pair(&done[b]);
             }
             tcgen05_commit_pair(&drained);
             wait_for(&drained, 0);
         }
     } else {
-        const uint32_t quarter = warp & 3u;
-        unsigned char* const out = tiles + S::kStage * kStages + quarter * 32 * kOutPitch;
+        const uint32_t quarter = warp & 3u, half = (warp - 2) >> 2;
+        unsigned char* const out = tiles + S::kStage * kStages + (warp - 2) * 32 * kOutPitch;
         uint32_t i = 0;
         for (uint32_t t = first; t < total; t += stride, ++i) {
             uint32_t rt, ct;
             tile_of(k, t, kBand, rt, ct);
-            const uint32_t b = i & 1, sums = tmem + b * S::kSecond + (quarter * 32 << 16), r = (rt * 2 + rank) * kRows + quarter * 32;
-            if (!wait_for(&done[b], (i / 2) & 1)) break;
+            const uint32_t b = i % S::kSums, c = half * (BN / 2);
+            if (!wait_for(&done[b], (i / S::kSums) & 1)) break;
             tcgen05_fence_after();
-            const auto free_sums = [&] {
+            store_columns_any<BN / 2>(k, out, tmem + b * BN + c + (quarter * 32 << 16), (rt * 2 + rank) * kRows + quarter * 32, ct * BN + c, [&] {
                 __syncwarp();
-                if (lane == 0) mbar_arrive_at(&free_[S::kOverlap ? 0 : b], 0);
-            };
-            if (k.type == ZCCL_BF16) store_tile<__nv_bfloat16, BN>(k, out, sums, r, ct * BN, b == 0, free_sums);
-            else if (k.type == ZCCL_F16) store_tile<__half, BN>(k, out, sums, r, ct * BN, b == 0, free_sums);
-            else store_tile<float, BN>(k, out, sums, r, ct * BN, b == 0, free_sums);
+                if (lane == 0) mbar_arrive_at(&free_[b], 0);
+            });
         }
     }
     __syncwarp();
@@ -533,7 +527,7 @@ cudaError_t product_device(const ProductDevice** out)
         if (e != cudaSuccess) return e;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)d.sms / 2 * 2);
-        cfg.blockDim = dim3(kProductThreads);
+        cfg.blockDim = dim3(kPairThreads);
         cfg.dynamicSmemBytes = PairShape<256>::kBytes;
         cudaLaunchAttribute attr;
         attr.id = cudaLaunchAttributeClusterDimension;
@@ -600,7 +594,7 @@ int launch_pair(const Sides& s, Product k, int pairs, cudaStream_t st)
     if (!operand_map(&r, s.r_codes, s.rows, k.depth_blocks, kRows) || !operand_map(&c, s.c_codes, s.cols, k.depth_blocks, BN / 2) ||
         !scales_map(&rs, k.r_scales, s.rows, k.depth_blocks, 1) || !scales_map(&cs, k.c_scales, s.cols, k.depth_blocks, PairShape<BN>::kBands)) return ZCCL_E_CUDA;
     const unsigned clusters = std::min(k.row_tiles * k.col_tiles, (unsigned)pairs);
-    return launched(launch_cluster(2, mx4_pair_kernel<BN>, dim3(2 * clusters), dim3(kProductThreads), PairShape<BN>::kBytes, st, r, c, rs, cs, k));
+    return launched(launch_cluster(2, mx4_pair_kernel<BN>, dim3(2 * clusters), dim3(kPairThreads), PairShape<BN>::kBytes, st, r, c, rs, cs, k));
 }
 
 bool aligned16(const void* p) { return p && ((uintptr_t)p & 15u) == 0; }
