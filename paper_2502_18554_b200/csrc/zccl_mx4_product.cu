@@ -118,6 +118,7 @@ __device__ __forceinline__ void store_rows(const Product& k, unsigned char* out,
     } else {
         constexpr uint32_t kAtOnce = 32 / kWidth;    // rows of a store
         const uint32_t at = lane % kWidth;
+#pragma unroll 8
         for (uint32_t row = lane / kWidth; row < high; row += kAtOnce)
             if (c + at < k.cols) y[(size_t)row * k.pitch + at] = *reinterpret_cast<const T*>(out + row * kOutPitch + at * sizeof(T));
     }
@@ -167,24 +168,64 @@ struct SplitShape {
     static_assert((228 * 1024 / kBytes) * kColumns <= 512, "clusters must not wait for each other's tensor memory");
 };
 
-// Four neighbouring sums, added over the parts in their order.  A warp's 32 lanes read 512 bytes in a row: what lies apart in another SM's memory comes
-// at a fraction of the speed.
-__device__ __forceinline__ float4 add_parts(uint32_t at, uint32_t parts)
+// N times four neighbouring sums, `step` bytes apart, added over the parts in their order.  All are asked for before the first is used: another SM's
+// memory is far away.  And a warp's 32 lanes read 512 bytes in a row: what lies apart there comes at a fraction of the speed.
+template <int PARTS, int N>
+__device__ __forceinline__ void add_parts(uint32_t at, uint32_t step, float4 (&sum)[N])
 {
-    float4 v[8], sum;
+    float4 v[PARTS][N];
 #pragma unroll
-    for (int p = 0; p < 8; ++p)
-        if (p < (int)parts) v[p] = peer_load4(at, p);
-    sum = v[0];
+    for (int p = 0; p < PARTS; ++p)
 #pragma unroll
-    for (int p = 1; p < 8; ++p)
-        if (p < (int)parts) {
-            sum.x += v[p].x;
-            sum.y += v[p].y;
-            sum.z += v[p].z;
-            sum.w += v[p].w;
+        for (int i = 0; i < N; ++i) v[p][i] = peer_load4(at + i * step, p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        sum[i] = v[0][i];
+#pragma unroll
+        for (int p = 1; p < PARTS; ++p) {
+            sum[i].x += v[p][i].x;
+            sum[i].y += v[p][i].y;
+            sum[i].z += v[p][i].z;
+            sum[i].w += v[p][i].w;
         }
-    return sum;
+    }
+}
+// The CTA's share of a tile's output; see mx4_split_kernel.
+template <int BN, int PARTS>
+__device__ __forceinline__ void store_share(const Product& k, uint32_t sums, uint32_t part, uint32_t r0, uint32_t c0)
+{
+    using S = SplitShape<BN>;
+    const uint32_t thread = threadIdx.x - 64, warp = thread >> 5, lane = thread & 31u;
+    if (k.across) {
+        constexpr int kMine = BN / 4 / PARTS ? BN / 4 / PARTS : 1, N = kMine < 4 ? kMine : 4;     // columns of a warp, and at a time
+        const uint32_t left = k.rows - min(k.rows, r0 + lane * 4);
+        for (uint32_t j = 0; j < (uint32_t)kMine; j += N) {
+            const uint32_t c = (part * kMine + j) * 4 + warp;                                     // and every fourth from here
+            if (c >= (uint32_t)BN || c0 + c >= k.cols) break;
+            float4 s[N];
+            add_parts<PARTS, N>(sums + (c * kRows + lane * 4) * 4, 4 * kRows * 4, s);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float four[4] = {s[i].x, s[i].y, s[i].z, s[i].w};
+                if (c0 + c + 4 * i < k.cols) store_four(k, (size_t)(c0 + c + 4 * i) * k.pitch + r0 + lane * 4, left, four);
+            }
+        }
+    } else {
+        constexpr uint32_t kQuads = BN / 4, kAtOnce = 128 / kQuads, kAll = kRows / kAtOnce, kSteps = kAll > PARTS ? kAll / PARTS : 1;   // rows that the four warps take at a time, and how often
+        constexpr int N = kSteps < 4 ? kSteps : 4;
+        const uint32_t c = thread % kQuads * 4, left = k.cols - min(k.cols, c0 + c);
+        for (uint32_t j = 0; j < kSteps; j += N) {
+            const uint32_t row = (part * kSteps + j) * kAtOnce + thread / kQuads;
+            if (part * kSteps + j >= kAll || r0 + (part * kSteps + j) * kAtOnce >= k.rows) break;
+            float4 s[N];
+            add_parts<PARTS, N>(sums + (row * S::kSumPitch + c) * 4, kAtOnce * S::kSumPitch * 4, s);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float four[4] = {s[i].x, s[i].y, s[i].z, s[i].w};
+                if (r0 + row + i * kAtOnce < k.rows) store_four(k, (size_t)(r0 + row + i * kAtOnce) * k.pitch + c0 + c, left, four);
+            }
+        }
+    }
 }
 
 template <int BN>
@@ -305,22 +346,11 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
     __syncwarp();
     cluster_sync();
     if (warp >= 2 && !(BN == 128 && parts == 1 && !k.across)) {
-        const uint32_t sums = smem_u32(tiles), r0 = rt * kRows, thread = threadIdx.x - 64;
-        if (k.across) {
-            for (uint32_t c = part * 4 + warp - 2; c < (uint32_t)BN && c0 + c < k.cols; c += parts * 4) {
-                const float4 s = add_parts(sums + (c * kRows + lane * 4) * 4, parts);
-                const float four[4] = {s.x, s.y, s.z, s.w};
-                store_four(k, (size_t)(c0 + c) * k.pitch + r0 + lane * 4, k.rows - min(k.rows, r0 + lane * 4), four);
-            }
-        } else {
-            constexpr uint32_t kQuads = BN / 4, kAtOnce = 128 / kQuads;      // rows that the four warps take at a time
-            const uint32_t c = thread % kQuads * 4;
-            for (uint32_t row = part * kAtOnce + thread / kQuads; row < kRows && r0 + row < k.rows; row += parts * kAtOnce) {
-                const float4 s = add_parts(sums + (row * S::kSumPitch + c) * 4, parts);
-                const float four[4] = {s.x, s.y, s.z, s.w};
-                store_four(k, (size_t)(r0 + row) * k.pitch + c0 + c, k.cols - min(k.cols, c0 + c), four);
-            }
-        }
+        const uint32_t sums = smem_u32(tiles), r0 = rt * kRows;
+        if (parts == 8) store_share<BN, 8>(k, sums, part, r0, c0);
+        else if (parts == 4) store_share<BN, 4>(k, sums, part, r0, c0);
+        else if (parts == 2) store_share<BN, 2>(k, sums, part, r0, c0);
+        else store_share<BN, 1>(k, sums, part, r0, c0);
     }
     __syncwarp();
     cluster_sync();                        // nobody leaves while its sums are still read
