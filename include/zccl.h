@@ -429,6 +429,15 @@ size_t zccl_mx4_scale_bytes(size_t rows, size_t cols);
 /* x [device] rows x cols, `pitch` elements from row to row, aligned to its element.  transpose != 0: the form of x's transpose
  * (cols x rows, blocks along x's columns), read without a copy. */
 int zccl_mx4_quantize(const void* x, int type, size_t rows, size_t cols, size_t pitch, int transpose, void* codes, void* scales, void* stream);
+/* The same for several matrices of one type in as few launches as they fit (eight to one): all that a layer's product or its gradient needs.  `jobs` [host] is read
+ * before the call returns; nothing has run where one is refused. */
+typedef struct {
+    const void* x;
+    size_t rows, cols, pitch;
+    int transpose;
+    void *codes, *scales;
+} zccl_mx4_job;
+int zccl_mx4_quantize_all(const zccl_mx4_job* jobs, int count, int type, void* stream);
 /* y [device] rows x cols, `pitch` elements from row to row: every x', rounded once to `type`. */
 int zccl_mx4_dequantize(const void* codes, const void* scales, size_t rows, size_t cols, void* y, int type, size_t pitch, void* stream);
 /*

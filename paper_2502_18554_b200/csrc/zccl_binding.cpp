@@ -328,6 +328,18 @@ PyObject* status_on(const at::Tensor& t, F&& f)
     }
 }
 
+// A list or tuple of tensors, kept alive by its caller.
+struct Tensors {
+    PyObject* seq = nullptr;
+    ~Tensors() { Py_XDECREF(seq); }
+    bool take(PyObject* o)
+    {
+        seq = PySequence_Fast(o, "expected a sequence of tensors");
+        return seq != nullptr;
+    }
+    size_t count() const { return seq ? (size_t)PySequence_Fast_GET_SIZE(seq) : 0; }
+    bool at(size_t i, const at::Tensor** t) const { return cuda_tensor(PySequence_Fast_GET_ITEM(seq, (Py_ssize_t)i), t); }
+};
 // ---- microscaled 4-bit floating point.  Outputs are allocated here, on the stream that the call runs on: through Python the small
 // allocations of a call took longer than its kernels.
 
@@ -373,6 +385,7 @@ struct Matrix {
         cols = (size_t)t->size(1);
         return true;
     }
+    zccl_mx4_job job(bool transpose, const Form& f) const { return {t->data_ptr(), rows, cols, pitch, transpose, f.codes.data_ptr(), f.scales.data_ptr()}; }
     int quantize(bool transpose, const Form& f, void* st) const
     {
         return zccl_mx4_quantize(t->data_ptr(), type, rows, cols, pitch, transpose, f.codes.data_ptr(), f.scales.data_ptr(), st);
@@ -426,6 +439,38 @@ PyObject* mx4_quantize(PyObject*, Args a, Py_ssize_t na)
         const int rc = x.quantize(transpose, f, place.st);
         if (rc != ZCCL_OK) return PyLong_FromLong(rc);
         return Py_BuildValue("NN", THPVariable_Wrap(f.codes), THPVariable_Wrap(f.scales));
+    });
+}
+
+// (matrices, transposes, stream) -> list of (codes, scales) or a status
+PyObject* mx4_quantize_all(PyObject*, Args a, Py_ssize_t na)
+{
+    if (!nargs_are(na, 3)) return nullptr;
+    Tensors xs, ts;
+    if (!xs.take(a[0]) || !ts.take(a[1])) return nullptr;
+    const size_t count = xs.count();
+    if (ts.count() != count) return refuse("lists of different lengths"), nullptr;
+    std::vector<Matrix> x(count);
+    std::vector<Form> f(count);
+    std::vector<zccl_mx4_job> jobs(count);
+    for (size_t i = 0; i < count; ++i) {
+        if (!x[i].take(PySequence_Fast_GET_ITEM(xs.seq, (Py_ssize_t)i))) return nullptr;
+        if (x[i].type != x[0].type || x[i].t->device() != x[0].t->device()) return refuse("all matrices of a call are of one type and on one device"), nullptr;
+    }
+    if (count == 0) return PyList_New(0);
+    return guarded([&]() -> PyObject* {
+        Place place;
+        if (!place.take(a[2], *x[0].t)) return nullptr;
+        for (size_t i = 0; i < count; ++i) {
+            const bool transpose = PyObject_IsTrue(PySequence_Fast_GET_ITEM(ts.seq, (Py_ssize_t)i)) == 1;
+            f[i] = transpose ? new_form(x[i].cols, x[i].rows, *x[0].t) : new_form(x[i].rows, x[i].cols, *x[0].t);
+            jobs[i] = x[i].job(transpose, f[i]);
+        }
+        const int rc = zccl_mx4_quantize_all(jobs.data(), (int)count, x[0].type, place.st);
+        if (rc != ZCCL_OK) return PyLong_FromLong(rc);
+        PyObject* const out = PyList_New((Py_ssize_t)count);
+        for (size_t i = 0; out && i < count; ++i) PyList_SET_ITEM(out, (Py_ssize_t)i, Py_BuildValue("NN", THPVariable_Wrap(f[i].codes), THPVariable_Wrap(f[i].scales)));
+        return out;
     });
 }
 
@@ -496,12 +541,13 @@ PyObject* mx4_linear(PyObject*, Args a, Py_ssize_t na)
         if (!place.take(Py_None, *x.t)) return nullptr;
         const Form f = new_form(x.rows, x.cols, *x.t);
         const at::Tensor y = new_matrix(x.rows, n, x.t->scalar_type(), *x.t);
-        int rc = ZCCL_OK;
+        int rc;
         if (na == 2) {
             held = new_form(n, x.cols, *x.t);
-            rc = w.quantize(false, held, place.st);
-        }
-        if (rc == ZCCL_OK)
+            const zccl_mx4_job both[2] = {w.job(false, held), x.job(false, f)};
+            rc = zccl_mx4_quantize_all(both, 2, x.type, place.st);
+            if (rc == ZCCL_OK) rc = multiply(f, x.rows, held, n, x.cols, y, place.st);
+        } else
             rc = zccl_mx4_linear(x.t->data_ptr(), x.type, x.rows, x.cols, x.pitch, held.codes.data_ptr(), held.scales.data_ptr(), n, f.codes.data_ptr(), f.scales.data_ptr(), y.data_ptr(), n, place.st);
         return wrapped(rc, y);
     });
@@ -521,21 +567,33 @@ PyObject* mx4_linear_backward(PyObject*, Args a, Py_ssize_t na)
         Place place;
         if (!place.take(Py_None, *x.t)) return nullptr;
         at::Tensor dx, dw;
-        int rc = ZCCL_OK;
+        Form xl, xr, wl, wr;
+        zccl_mx4_job jobs[4];
+        int count = 0;
         if (want_x) {
-            const Form l = new_form(m, n, *x.t), r = new_form(k, n, *x.t);
+            xl = new_form(m, n, *x.t);
+            xr = new_form(k, n, *x.t);
             dx = new_matrix(m, k, x.t->scalar_type(), *x.t);
-            rc = dy.quantize(false, l, place.st);
-            if (rc == ZCCL_OK) rc = w.quantize(true, r, place.st);
-            if (rc == ZCCL_OK) rc = multiply(l, m, r, k, n, dx, place.st);
+            jobs[count++] = dy.job(false, xl);
+            jobs[count++] = w.job(true, xr);
         }
-        if (want_w && rc == ZCCL_OK) {
-            const Form l = new_form(n, m, *x.t), r = new_form(k, m, *x.t);
+        if (want_w) {
+            wl = new_form(n, m, *x.t);
+            wr = new_form(k, m, *x.t);
             dw = new_matrix(n, k, w.t->scalar_type(), *x.t);
-            rc = dy.quantize(true, l, place.st);
-            if (rc == ZCCL_OK) rc = x.quantize(true, r, place.st);
-            if (rc == ZCCL_OK) rc = multiply(l, n, r, k, m, dw, place.st);
+            jobs[count++] = dy.job(true, wl);
+            jobs[count++] = x.job(true, wr);
         }
+        int rc = ZCCL_OK;
+        if (dy.type == x.type && w.type == x.type) rc = zccl_mx4_quantize_all(jobs, count, x.type, place.st);
+        else {
+            if (want_x) rc = dy.quantize(false, xl, place.st);
+            if (want_x && rc == ZCCL_OK) rc = w.quantize(true, xr, place.st);
+            if (want_w && rc == ZCCL_OK) rc = dy.quantize(true, wl, place.st);
+            if (want_w && rc == ZCCL_OK) rc = x.quantize(true, wr, place.st);
+        }
+        if (want_x && rc == ZCCL_OK) rc = multiply(xl, m, xr, k, n, dx, place.st);
+        if (want_w && rc == ZCCL_OK) rc = multiply(wl, n, wr, k, m, dw, place.st);
         if (rc != ZCCL_OK) return PyLong_FromLong(rc);
         Py_INCREF(Py_None);
         Py_INCREF(Py_None);
@@ -547,18 +605,6 @@ PyObject* mx4_linear_backward(PyObject*, Args a, Py_ssize_t na)
     });
 }
 
-// A list or tuple of tensors, kept alive by its caller.
-struct Tensors {
-    PyObject* seq = nullptr;
-    ~Tensors() { Py_XDECREF(seq); }
-    bool take(PyObject* o)
-    {
-        seq = PySequence_Fast(o, "expected a sequence of tensors");
-        return seq != nullptr;
-    }
-    size_t count() const { return seq ? (size_t)PySequence_Fast_GET_SIZE(seq) : 0; }
-    bool at(size_t i, const at::Tensor** t) const { return cuda_tensor(PySequence_Fast_GET_ITEM(seq, (Py_ssize_t)i), t); }
-};
 // Entry i of a list that belongs to `like`: contiguous, of type `dt`, `n` elements, on the same device.
 bool entry(const Tensors& list, size_t i, c10::ScalarType dt, size_t n, const at::Tensor& like, const at::Tensor** t)
 {
@@ -715,7 +761,7 @@ PyMethodDef methods[] = {
     FAST(compress), FAST(decompress), FAST(hop), FAST(compress_f64), FAST(decompress_f64), FAST(compress_tiled), FAST(decompress_tiled), FAST(sim_allreduce),
     {"sim_allgather", (PyCFunction)(void (*)(void))sim<zccl_sim_allgather>, METH_FASTCALL, nullptr},
     {"sim_reduce_scatter", (PyCFunction)(void (*)(void))sim<zccl_sim_reduce_scatter>, METH_FASTCALL, nullptr},
-    FAST(mx4_sizes), FAST(mx4_quantize), FAST(mx4_dequantize), FAST(mx4_matmul), FAST(mx4_linear), FAST(mx4_linear_backward), FAST(adamw), FAST(grad_norm),
+    FAST(mx4_sizes), FAST(mx4_quantize), FAST(mx4_quantize_all), FAST(mx4_dequantize), FAST(mx4_matmul), FAST(mx4_linear), FAST(mx4_linear_backward), FAST(adamw), FAST(grad_norm),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_zccl", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

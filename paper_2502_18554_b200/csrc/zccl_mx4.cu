@@ -73,24 +73,46 @@ __device__ __forceinline__ void load8(const T* __restrict__ row, uint32_t at, ui
     }
 }
 
+// One matrix to quantise: its sizes, how its kernel goes round it (rows), and the launch's CTA that it begins at.
+enum MxKind : uint32_t { kMxRowsStrips, kMxRows, kMxRowsPlain, kMxColumns, kMxColumnsPlain };
+struct MxJob {
+    const void* x;
+    void* codes;
+    unsigned char* scales;
+    size_t pitch;
+    uint32_t rows, cols, blocks, groups;
+    uint32_t strips, total, work, step_row, step_strip;   // rows: see Rounds; `work`: CTAs that quantise, those behind fill scales up
+    uint32_t across;                                      // columns: CTAs to a band of eight blocks
+    uint32_t first;
+    MxKind kind;
+};
+constexpr int kMxJobs = 8;
+struct MxJobs {
+    MxJob job[kMxJobs];
+    int count;
+};
+
 // Rows: 16 lanes take STRIP groups of 128 neighbouring elements of a row (a group: four blocks, one word of scales), a lane
 // eight elements of each, so loads are 16 bytes a lane and codes leave as whole lines.  Blocks behind the last are quantised as zeros. CTAs from
 // `work` on write the scales of the rows that fill the last band up, a word a thread.
 // Bound by memory where it is large (8192 x 8192 bf16: 30.5 us, 5.6 TB/s); with one group at a time the indexes cost more instructions than the elements
 // (23 to an element, 52.5 us).
 template <class T, bool VEC, int STRIP>
-__global__ void __launch_bounds__(kMxThreads) mx_quantize_rows_kernel(const T* __restrict__ x, uint32_t rows, uint32_t cols, size_t pitch,
-                                                                       uint32_t blocks, uint32_t groups, uint32_t strips, uint32_t total, uint32_t work, uint32_t step_row,
-                                                                       uint32_t step_strip, uint32_t* __restrict__ codes, unsigned char* __restrict__ scales)
+__device__ __forceinline__ void quantize_rows(const MxJob& job, uint32_t cta)
 {
-    pdl_enter();
-    if (blockIdx.x >= work) {
-        const uint32_t i = (blockIdx.x - work) * kMxThreads + threadIdx.x, r = rows + i / groups;
+    const T* __restrict__ const x = (const T*)job.x;
+    const uint32_t rows = job.rows, cols = job.cols, blocks = job.blocks, groups = job.groups, strips = job.strips, total = job.total, work = job.work;
+    const uint32_t step_row = job.step_row, step_strip = job.step_strip;
+    const size_t pitch = job.pitch;
+    uint32_t* __restrict__ const codes = (uint32_t*)job.codes;
+    unsigned char* __restrict__ const scales = job.scales;
+    if (cta >= work) {
+        const uint32_t i = (cta - work) * kMxThreads + threadIdx.x, r = rows + i / groups;
         if ((rows - 1) / kMxBand == r / kMxBand) *reinterpret_cast<uint32_t*>(scales + mx_scale_at(r, i % groups, groups)) = 0u;
         return;
     }
     const uint32_t sub = threadIdx.x & 15u;
-    uint32_t u = blockIdx.x * (kMxThreads / 16) + (threadIdx.x >> 4);
+    uint32_t u = cta * (kMxThreads / 16) + (threadIdx.x >> 4);
     uint32_t r = u / strips, strip = u - r * strips;
     const uint32_t stride = work * (kMxThreads / 16);
     // whole warps go round together: the last round's idle half takes part in the exchanges with zeros
@@ -142,15 +164,22 @@ __global__ void __launch_bounds__(kMxThreads) mx_quantize_rows_kernel(const T* _
 // 128 bytes and words of scales.
 constexpr int kColumnWarps = 8, kColumnWidth = 64;
 constexpr int kColumnPad = kColumnWarps + 1;   // sixteen-byte pieces of a column in shared memory: an odd number keeps the writes of eight lanes apart
+struct ColumnsShared {
+    uint4 codes[kColumnWidth][kColumnPad];
+    __align__(8) unsigned char scales[kColumnWidth][kColumnWarps];
+};
 template <class T, bool VEC>
-__global__ void __launch_bounds__(kColumnWarps * 32) mx_quantize_columns_kernel(const T* __restrict__ x, uint32_t rows, uint32_t cols, size_t pitch, uint32_t blocks,
-                                                                                 uint32_t groups, uint32_t across, uint4* __restrict__ codes, unsigned char* __restrict__ scales)
+__device__ __forceinline__ void quantize_columns(const MxJob& job, uint32_t cta, ColumnsShared& sh)
 {
-    pdl_enter();
-    __shared__ uint4 sh_codes[kColumnWidth][kColumnPad];
-    __shared__ __align__(8) unsigned char sh_scales[kColumnWidth][kColumnWarps];
+    const T* __restrict__ const x = (const T*)job.x;
+    const uint32_t rows = job.rows, cols = job.cols, blocks = job.blocks, groups = job.groups, across = job.across;
+    const size_t pitch = job.pitch;
+    uint4* __restrict__ const codes = (uint4*)job.codes;
+    unsigned char* __restrict__ const scales = job.scales;
+    auto& sh_codes = sh.codes;
+    auto& sh_scales = sh.scales;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
-    const uint32_t band = blockIdx.x / across, c0 = (blockIdx.x - band * across) * kColumnWidth;
+    const uint32_t band = cta / across, c0 = (cta - band * across) * kColumnWidth;
     const uint32_t c = c0 + lane * 2, b = band * kColumnWarps + warp, r0 = b * kMxBlock;
     MxTwo<T> v[kMxBlock];
     if (VEC && c0 + kColumnWidth <= cols && r0 + kMxBlock <= rows) {
@@ -201,7 +230,43 @@ __global__ void __launch_bounds__(kColumnWarps * 32) mx_quantize_columns_kernel(
     }
 }
 
-// Back: lanes as in mx_quantize_rows_kernel.  Where rows do not begin on 16-byte boundaries a lane takes every sixteenth element of a group instead of
+template <class T, MxKind KIND>
+__device__ __forceinline__ void quantize_one(const MxJob& job, uint32_t cta, ColumnsShared& sh)
+{
+    if constexpr (KIND == kMxRowsStrips) quantize_rows<T, true, 4>(job, cta);
+    else if constexpr (KIND == kMxRows) quantize_rows<T, true, 1>(job, cta);
+    else if constexpr (KIND == kMxRowsPlain) quantize_rows<T, false, 1>(job, cta);
+    else if constexpr (KIND == kMxColumns) quantize_columns<T, true>(job, cta, sh);
+    else quantize_columns<T, false>(job, cta, sh);
+}
+// One matrix: a kernel for each way, of which rows need half the registers of columns.
+template <class T, MxKind KIND>
+__global__ void __launch_bounds__(kMxThreads) mx_quantize_kernel(const __grid_constant__ MxJob job)
+{
+    __shared__ ColumnsShared sh;
+    pdl_enter();
+    quantize_one<T, KIND>(job, blockIdx.x, sh);
+}
+// Several: the small ones of a layer would each take as long as a launch.
+template <class T>
+__global__ void __launch_bounds__(kMxThreads) mx_quantize_all_kernel(const __grid_constant__ MxJobs jobs)
+{
+    __shared__ ColumnsShared sh;
+    pdl_enter();
+    int i = 0;
+    while (i + 1 < jobs.count && jobs.job[i + 1].first <= blockIdx.x) ++i;
+    const MxJob& job = jobs.job[i];
+    const uint32_t cta = blockIdx.x - job.first;
+    switch (job.kind) {
+        case kMxRowsStrips: quantize_one<T, kMxRowsStrips>(job, cta, sh); break;
+        case kMxRows: quantize_one<T, kMxRows>(job, cta, sh); break;
+        case kMxRowsPlain: quantize_one<T, kMxRowsPlain>(job, cta, sh); break;
+        case kMxColumns: quantize_one<T, kMxColumns>(job, cta, sh); break;
+        default: quantize_one<T, kMxColumnsPlain>(job, cta, sh); break;
+    }
+}
+
+// Back: lanes as in quantize_rows.  Where rows do not begin on 16-byte boundaries a lane takes every sixteenth element of a group instead of
 // eight neighbours, so that a store is still one run.
 template <class T, bool VEC, int STRIP>
 __global__ void __launch_bounds__(kMxThreads) mx_dequantize_kernel(const uint32_t* __restrict__ codes, const unsigned char* __restrict__ scales, uint32_t rows,
@@ -285,34 +350,70 @@ Rounds rounds_of(size_t rows, size_t groups, int strip)
 constexpr size_t kStripWork = 1 << 15;
 bool strips_pay(size_t rows, size_t groups) { return groups >= 4 && rows * groups >= kStripWork; }
 
-template <class T, bool VEC>
-cudaError_t launch_rows(const T* x, size_t rows, size_t cols, size_t pitch, void* codes, void* scales, cudaStream_t st)
+int launched(cudaError_t e)
 {
-    const size_t blocks = mx_blocks(cols), groups = mx_groups(cols), padding = (mx_bands(rows) * kMxBand - rows) * groups;
-    const bool four = strips_pay(rows, groups);
-    const Rounds k = rounds_of(rows, groups, four ? 4 : 1);
-    const unsigned fill = (unsigned)((padding + kMxThreads - 1) / kMxThreads);
-    return launch_k(four ? mx_quantize_rows_kernel<T, VEC, 4> : mx_quantize_rows_kernel<T, VEC, 1>, dim3(k.ctas + fill), dim3(kMxThreads), 0, st, x, (uint32_t)rows, (uint32_t)cols,
-                    pitch, (uint32_t)blocks, (uint32_t)groups, k.strips, k.total, k.ctas, k.step_row, k.step_strip, (uint32_t*)codes, (unsigned char*)scales);
-}
-
-template <class T>
-int quantize(const T* x, size_t rows, size_t cols, size_t pitch, bool transpose, void* codes, void* scales, cudaStream_t st)
-{
-    const uintptr_t at = (uintptr_t)x;
-    cudaError_t e;
-    if (transpose) {
-        const size_t blocks = mx_blocks(rows), groups = mx_groups(rows), across = mx_bands(cols) * (kMxBand / kColumnWidth), down = (blocks + kColumnWarps - 1) / kColumnWarps;
-        if (down * across > kMxMaxGroups) return ZCCL_E_ARG;
-        const bool vec = at % (2 * sizeof(T)) == 0 && pitch % 2 == 0;
-        e = launch_k(vec ? mx_quantize_columns_kernel<T, true> : mx_quantize_columns_kernel<T, false>, dim3((unsigned)(down * across)), dim3(kColumnWarps * 32), 0, st,
-                     x, (uint32_t)rows, (uint32_t)cols, pitch, (uint32_t)blocks, (uint32_t)groups, (uint32_t)across, (uint4*)codes, (unsigned char*)scales);
-    } else {
-        if (mx_bands(rows) * kMxBand * mx_groups(cols) > kMxMaxGroups) return ZCCL_E_ARG;
-        e = at % 16 == 0 && pitch * sizeof(T) % 16 == 0 ? launch_rows<T, true>(x, rows, cols, pitch, codes, scales, st) : launch_rows<T, false>(x, rows, cols, pitch, codes, scales, st);
-    }
     if (e == cudaSuccess) count_launches(1);
     return e == cudaSuccess ? ZCCL_OK : ZCCL_E_CUDA;
+}
+// How a matrix is gone about; returns its CTAs (0: more than can be counted).
+unsigned plan(const zccl_mx4_job& j, size_t element, MxJob& to)
+{
+    const uintptr_t at = (uintptr_t)j.x;
+    to = MxJob{};
+    to.x = j.x;
+    to.codes = j.codes;
+    to.scales = (unsigned char*)j.scales;
+    to.pitch = j.pitch;
+    to.rows = (uint32_t)j.rows;
+    to.cols = (uint32_t)j.cols;
+    const size_t along = j.transpose ? j.rows : j.cols, groups = mx_groups(along);
+    to.blocks = (uint32_t)mx_blocks(along);
+    to.groups = (uint32_t)groups;
+    if (j.transpose) {
+        const size_t across = mx_bands(j.cols) * (kMxBand / kColumnWidth), ctas = (to.blocks + kColumnWarps - 1) / kColumnWarps * across;
+        to.across = (uint32_t)across;
+        to.kind = at % (2 * element) == 0 && j.pitch % 2 == 0 ? kMxColumns : kMxColumnsPlain;
+        return ctas > kMxMaxGroups ? 0u : (unsigned)ctas;
+    }
+    if (mx_bands(j.rows) * kMxBand * groups > kMxMaxGroups) return 0u;
+    to.kind = at % 16 || j.pitch * element % 16 ? kMxRowsPlain : strips_pay(j.rows, groups) ? kMxRowsStrips : kMxRows;
+    const Rounds k = rounds_of(j.rows, groups, to.kind == kMxRowsStrips ? 4 : 1);
+    to.strips = k.strips;
+    to.total = k.total;
+    to.work = k.ctas;
+    to.step_row = k.step_row;
+    to.step_strip = k.step_strip;
+    return k.ctas + (unsigned)(((mx_bands(j.rows) * kMxBand - j.rows) * groups + kMxThreads - 1) / kMxThreads);
+}
+template <class T>
+int quantize_all(const zccl_mx4_job* jobs, int count, cudaStream_t st)
+{
+    MxJobs list;
+    for (int at = 0; at < count;) {
+        unsigned ctas = 0;
+        list.count = 0;
+        for (; at < count && list.count < kMxJobs; ++at) {
+            if (jobs[at].rows == 0 || jobs[at].cols == 0) continue;
+            MxJob& job = list.job[list.count];
+            const unsigned mine = plan(jobs[at], sizeof(T), job);
+            if (mine == 0) return ZCCL_E_ARG;
+            if (ctas > kMxMaxGroups - mine) break;
+            job.first = ctas;
+            ctas += mine;
+            ++list.count;
+        }
+        if (list.count == 0) continue;
+        int rc;
+        if (list.count > 1) rc = launched(launch_k(mx_quantize_all_kernel<T>, dim3(ctas), dim3(kMxThreads), 0, st, list));
+        else {
+            const auto kernel = list.job[0].kind == kMxRowsStrips ? mx_quantize_kernel<T, kMxRowsStrips> : list.job[0].kind == kMxRows ? mx_quantize_kernel<T, kMxRows>
+                                : list.job[0].kind == kMxRowsPlain ? mx_quantize_kernel<T, kMxRowsPlain> : list.job[0].kind == kMxColumns ? mx_quantize_kernel<T, kMxColumns>
+                                                                                                                                           : mx_quantize_kernel<T, kMxColumnsPlain>;
+            rc = launched(launch_k(kernel, dim3(ctas), dim3(kMxThreads), 0, st, list.job[0]));
+        }
+        if (rc != ZCCL_OK) return rc;
+    }
+    return ZCCL_OK;
 }
 
 template <class T, bool VEC>
@@ -331,8 +432,7 @@ int dequantize(const void* codes, const void* scales, size_t rows, size_t cols, 
     if (rows * mx_groups(cols) > kMxMaxGroups) return ZCCL_E_ARG;
     const bool vec = (uintptr_t)y % 16 == 0 && pitch * sizeof(T) % 16 == 0;
     const cudaError_t e = vec ? launch_back<T, true>(codes, scales, rows, cols, y, pitch, st) : launch_back<T, false>(codes, scales, rows, cols, y, pitch, st);
-    if (e == cudaSuccess) count_launches(1);
-    return e == cudaSuccess ? ZCCL_OK : ZCCL_E_CUDA;
+    return launched(e);
 }
 
 constexpr size_t kMost = 0x7FFFFF00u;   // rows and columns are counted in 32 bits
@@ -355,14 +455,20 @@ size_t zccl_mx4_code_bytes(size_t rows, size_t cols) { return rows * mx_blocks(c
 
 size_t zccl_mx4_scale_bytes(size_t rows, size_t cols) { return mx_bands(rows) * mx_groups(cols) * kMxTileBytes; }
 
+int zccl_mx4_quantize_all(const zccl_mx4_job* jobs, int count, int type, void* stream)
+{
+    if (count < 0 || (count && !jobs) || type < ZCCL_F32 || type > ZCCL_F16) return ZCCL_E_ARG;
+    for (int i = 0; i < count; ++i)
+        if (jobs[i].rows && jobs[i].cols && (!matrix_ok(jobs[i].x, type, jobs[i].rows, jobs[i].cols, jobs[i].pitch) || !aligned(jobs[i].codes, 16) || !aligned(jobs[i].scales, 16)))
+            return ZCCL_E_ARG;
+    cudaStream_t st = (cudaStream_t)stream;
+    return type == ZCCL_F32 ? quantize_all<float>(jobs, count, st) : type == ZCCL_BF16 ? quantize_all<__nv_bfloat16>(jobs, count, st) : quantize_all<__half>(jobs, count, st);
+}
+
 int zccl_mx4_quantize(const void* x, int type, size_t rows, size_t cols, size_t pitch, int transpose, void* codes, void* scales, void* stream)
 {
-    if (rows == 0 || cols == 0) return type < ZCCL_F32 || type > ZCCL_F16 ? ZCCL_E_ARG : ZCCL_OK;
-    if (!matrix_ok(x, type, rows, cols, pitch) || !aligned(codes, 16) || !aligned(scales, 16)) return ZCCL_E_ARG;
-    cudaStream_t st = (cudaStream_t)stream;
-    if (type == ZCCL_F32) return quantize((const float*)x, rows, cols, pitch, transpose != 0, codes, scales, st);
-    if (type == ZCCL_BF16) return quantize((const __nv_bfloat16*)x, rows, cols, pitch, transpose != 0, codes, scales, st);
-    return quantize((const __half*)x, rows, cols, pitch, transpose != 0, codes, scales, st);
+    const zccl_mx4_job job{x, rows, cols, pitch, transpose, codes, scales};
+    return zccl_mx4_quantize_all(&job, 1, type, stream);
 }
 
 int zccl_mx4_dequantize(const void* codes, const void* scales, size_t rows, size_t cols, void* y, int type, size_t pitch, void* stream)

@@ -629,6 +629,17 @@ int launch_pair(const Sides& s, Product k, int pairs, cudaStream_t st)
 
 bool aligned16(const void* p) { return p && ((uintptr_t)p & 15u) == 0; }
 
+// In how many pieces, a power of two up to 8, the contraction goes.  Narrow tiles: as many as there is room for at two CTAs to an SM.  Tiles of 128 x 128: at
+// one to an SM, and not at all where that saves fewer than seven stages, since joining their sums takes 2.6 us and a stage 0.4 us (measured, in
+// a graph: 512^3 4.0 us in one piece and 6.1 us in two; 300 x 300 x 16384 28.7 us in one, 9.5 us in eight; 128 x 4096 x 4096 11.8 us in one,
+// 7.5 us in four and 10.6 us in eight at two to an SM).
+unsigned parts_of(size_t tiles, size_t depth_tiles, size_t sms, bool wide)
+{
+    unsigned parts = 1;
+    while (parts < 8 && parts * 2 <= depth_tiles && tiles * parts * 2 <= (wide ? 1 : 2) * sms) parts *= 2;
+    return wide && depth_tiles - up(depth_tiles, parts) < 7 ? 1 : parts;
+}
+
 // `weights_ready`: B was complete before the kernel in front on the stream started.
 int multiply(const void* a_codes, const void* a_scales, size_t m, const void* b_codes, const void* b_scales, size_t n, size_t k, void* y, int type, size_t pitch, bool weights_ready, void* stream)
 {
@@ -663,9 +674,7 @@ int multiply(const void* a_codes, const void* a_scales, size_t m, const void* b_
     p.cols = (uint32_t)sides.cols;
     const size_t sms = (size_t)dev->sms, depth_tiles = up(p.depth_blocks, 8), tiles = up(sides.rows, kRows) * up(sides.cols, 128);
     if (tiles <= sms || sides.cols <= 128) {
-        // the contraction in as many pieces as the SMs take at two to an SM
-        unsigned parts = 1;
-        while (parts < 8 && parts * 2 <= depth_tiles && tiles * parts * 2 <= 2 * sms) parts *= 2;
+        const unsigned parts = parts_of(tiles, depth_tiles, sms, sides.cols > 64);
         if (sides.cols <= 16) return launch_split<16>(sides, p, parts, st);
         if (sides.cols <= 32) return launch_split<32>(sides, p, parts, st);
         if (sides.cols <= 64) return launch_split<64>(sides, p, parts, st);

@@ -54,13 +54,21 @@ def quantize(x: torch.Tensor, transpose: bool = False, out: Mx4 | None = None, s
     `transpose` the form of x's transpose, blocks along x's columns."""
     if x.dim() != 2:
         raise ValueError("expected a matrix")
-    cols, rows = x.shape if transpose else reversed(x.shape)
+    rows, cols = reversed(x.shape) if transpose else x.shape
     if out is None:
         return Mx4(*_value(z.native().mx4_quantize(x, transpose, None, None, stream), "zccl_mx4_quantize"), rows, cols)
     if (out.rows, out.cols) != (rows, cols):
         raise ValueError(f"expected the form of a matrix [{rows}, {cols}], got one of [{out.rows}, {out.cols}]")
     _value(z.native().mx4_quantize(x, transpose, out.codes, out.scales, stream), "zccl_mx4_quantize")
     return out
+
+
+def quantize_all(matrices, transpose=None, stream=None) -> list[Mx4]:
+    """quantize of several matrices of one type, in as few launches as they fit; `transpose`: whether, for each (default: none)."""
+    matrices = list(matrices)
+    transpose = [False] * len(matrices) if transpose is None else list(transpose)
+    forms = _value(z.native().mx4_quantize_all(matrices, transpose, stream), "zccl_mx4_quantize_all")
+    return [Mx4(codes, scales, *(reversed(x.shape) if t else x.shape)) for (codes, scales), x, t in zip(forms, matrices, transpose)]
 
 
 def dequantize(q: Mx4, dtype: torch.dtype = torch.float32, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:

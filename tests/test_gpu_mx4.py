@@ -133,6 +133,25 @@ def test_streams_graphs_and_buffers_that_are_given(mx):
     assert torch.equal(out.codes, mx.quantize(x).codes) and torch.equal(y, mx.dequantize(mx.quantize(x)))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_several_matrices_in_one_call(mx, dtype):
+    """Of every kind (rows in strips, rows, rows and columns on no boundary, columns), more than one launch takes, empty ones between them."""
+    shapes = [(300, 520, False), (1, 32, False), (70, 131, False), (65, 96, True), (33, 77, True), (0, 64, False), (5, 0, True), (513, 1024, False), (1000, 8, True), (2, 4096, False), (129, 130, True)]
+    xs = [data(r, c, dtype, i) for i, (r, c, _) in enumerate(shapes)]
+    xs[7] = data(513, 8192, dtype, 7)                       # enough groups for strips of four
+    forms = mx.quantize_all([x.cuda() for x in xs], [t for _, _, t in shapes])
+    assert len(forms) == len(xs)
+    for x, (_, _, t), q in zip(xs, shapes, forms):
+        assert (q.rows, q.cols) == (tuple(reversed(x.shape)) if t else tuple(x.shape))
+        if x.numel():
+            check(mx, x, t, q)
+    assert mx.quantize_all([]) == []
+    with pytest.raises(ValueError):
+        mx.quantize_all([xs[0].cuda(), xs[1].cuda().double()])
+    with pytest.raises(ValueError):
+        mx.quantize_all([xs[0].cuda()], [True, False])
+
+
 def test_refusals(mx):
     x = torch.zeros(4, 64, device="cuda")
     q = mx.quantize(x)
