@@ -95,8 +95,9 @@ struct MxJobs {
 // Rows: 16 lanes take STRIP groups of 128 neighbouring elements of a row (a group: four blocks, one word of scales), a lane
 // eight elements of each, so loads are 16 bytes a lane and codes leave as whole lines.  Blocks behind the last are quantised as zeros. CTAs from
 // `work` on write the scales of the rows that fill the last band up, a word a thread.
-// Bound by memory where it is large (8192 x 8192 bf16: 30.5 us, 5.6 TB/s); with one group at a time the indexes cost more instructions than the elements
-// (23 to an element, 52.5 us).
+// Bound by memory where it is large (8192 x 8192 bf16: 30 us, 5.7 TB/s); with one group at a time the indexes cost more instructions than the elements
+// (23 to an element, 52.5 us).  Rows that do not begin on 16-byte boundaries are loaded element by element and take twice as long (16384 x 4097: 65 us; cutting them out
+// of aligned pieces took as long).
 template <class T, bool VEC, int STRIP>
 __device__ __forceinline__ void quantize_rows(const MxJob& job, uint32_t cta)
 {
@@ -235,13 +236,15 @@ __device__ __forceinline__ void quantize_one(const MxJob& job, uint32_t cta, Col
 {
     if constexpr (KIND == kMxRowsStrips) quantize_rows<T, true, 4>(job, cta);
     else if constexpr (KIND == kMxRows) quantize_rows<T, true, 1>(job, cta);
-    else if constexpr (KIND == kMxRowsPlain) quantize_rows<T, false, 1>(job, cta);
+    else if constexpr (KIND == kMxRowsPlain) quantize_rows<T, false, 4>(job, cta);
     else if constexpr (KIND == kMxColumns) quantize_columns<T, true>(job, cta, sh);
     else quantize_columns<T, false>(job, cta, sh);
 }
-// One matrix: a kernel for each way, of which rows need half the registers of columns.
+// One matrix: a kernel for each way, of which rows need half the registers of columns.  Columns wait for memory, so they take as many CTAs to an SM as a few
+// spilled registers buy: whole pairs of 16-bit elements four (8192 x 8192 bf16: 26.7 us; three 28.1, two 34.1), the others three (16384 x 4097 bf16:
+// 45.9 us; four 63.3, two 55.5).
 template <class T, MxKind KIND>
-__global__ void __launch_bounds__(kMxThreads) mx_quantize_kernel(const __grid_constant__ MxJob job)
+__global__ void __launch_bounds__(kMxThreads, KIND < kMxColumns ? 1 : KIND == kMxColumns && sizeof(T) == 2 ? 4 : 3) mx_quantize_kernel(const __grid_constant__ MxJob job)
 {
     __shared__ ColumnsShared sh;
     pdl_enter();
@@ -249,7 +252,7 @@ __global__ void __launch_bounds__(kMxThreads) mx_quantize_kernel(const __grid_co
 }
 // Several: the small ones of a layer would each take as long as a launch.
 template <class T>
-__global__ void __launch_bounds__(kMxThreads) mx_quantize_all_kernel(const __grid_constant__ MxJobs jobs)
+__global__ void __launch_bounds__(kMxThreads, sizeof(T) == 2 ? 4 : 3) mx_quantize_all_kernel(const __grid_constant__ MxJobs jobs)
 {
     __shared__ ColumnsShared sh;
     pdl_enter();
@@ -266,67 +269,64 @@ __global__ void __launch_bounds__(kMxThreads) mx_quantize_all_kernel(const __gri
     }
 }
 
-// Back: lanes as in quantize_rows.  Where rows do not begin on 16-byte boundaries a lane takes every sixteenth element of a group instead of
-// eight neighbours, so that a store is still one run.
-template <class T, bool VEC, int STRIP>
+// Back: 16 lanes take STRIP runs of 128 neighbouring elements of a row, a lane as many as make 16 bytes of the output at a time, so a store of the
+// 16 lanes is one run of whole sectors.  Rows that begin on 16 bytes (WIDE) have their runs begin there; elsewhere runs begin at the row's first 16-byte
+// boundary, `head` elements in, and a lane's elements are cut out of two words of codes and may lie in two blocks; the head and the end are stored one by one
+// (16384 x 4097 bf16: 59 us against 73.6 us one by one; 8192 x 8192, on boundaries: 27.5 us, 6.2 TB/s).
+template <class T, bool WIDE, int STRIP>
 __global__ void __launch_bounds__(kMxThreads) mx_dequantize_kernel(const uint32_t* __restrict__ codes, const unsigned char* __restrict__ scales, uint32_t rows,
                                                                     uint32_t cols, uint32_t blocks, uint32_t groups, uint32_t strips, uint32_t total, uint32_t step_row,
                                                                     uint32_t step_strip, T* __restrict__ y, size_t pitch)
 {
     pdl_enter();
+    constexpr uint32_t kPer = 16 / sizeof(T), kTurns = kMxGroup / 16 / kPer;     // elements of a lane at a time, and how often to a run
     const uint32_t sub = threadIdx.x & 15u;
     uint32_t u = blockIdx.x * (kMxThreads / 16) + (threadIdx.x >> 4);
     uint32_t r = u / strips, strip = u - r * strips;
     const uint32_t stride = gridDim.x * (kMxThreads / 16);
     for (; u < total; u += stride) {
-        const uint32_t g0 = strip * STRIP;
-        const unsigned char* const scale = scales + mx_scale_at(r, g0, groups);
         T* const row = y + (size_t)r * pitch;
-        if (VEC) {
-            const uint32_t at = g0 * kMxGroup + sub * 8;
-            const uint32_t* const in = codes + ((size_t)r * blocks + (at >> 5)) * 4 + (sub & 3u);
-            uint32_t w[STRIP], s[STRIP];
+        const uint32_t* const in = codes + (size_t)r * blocks * 4;
+        const auto scale_at = [&](uint32_t block) { return scales[mx_scale_at(r, block >> 2, groups) + (block & 3u)]; };
+        const uint32_t head = WIDE ? 0u : (16u - (uint32_t)((uintptr_t)row & 15u)) % 16u / (uint32_t)sizeof(T);
+        const uint32_t from = head + strip * STRIP * kMxGroup + sub * kPer;
+        uint32_t w[STRIP * kTurns], s[STRIP * kTurns], s2[WIDE ? 1 : STRIP * kTurns];
 #pragma unroll
-            for (int j = 0; j < STRIP; ++j)
-                if (at + j * kMxGroup < cols) {
-                    w[j] = __ldcs(in + 16 * j);
-                    s[j] = scale[j * kMxTileBytes + (sub >> 2)];
-                }
-#pragma unroll
-            for (int j = 0; j < STRIP; ++j) {
-                const uint32_t here = at + j * kMxGroup;
-                if (here >= cols) break;
-                float v[8];
-                mx_decode8(w[j], mx_scale(s[j]), v);
-                constexpr int kPer = 16 / sizeof(T);
-                if (here + 8 <= cols) {
-#pragma unroll
-                    for (int i = 0; i < 8 / kPer; ++i) {
-                        MxPack<T> p;
-#pragma unroll
-                        for (int q = 0; q < kPer; ++q) p.v[q] = mx_round<T>(v[kPer * i + q]);
-                        reinterpret_cast<uint4*>(row + here)[i] = *reinterpret_cast<const uint4*>(&p);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (here + i < cols) row[here + i] = mx_round<T>(v[i]);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < STRIP; ++j) {
-                const uint32_t at = (g0 + j) * kMxGroup;
-                if (at >= cols) break;
-                const unsigned char* const in = reinterpret_cast<const unsigned char*>(codes) + ((size_t)r * blocks + (at >> 5)) * 16;
-                const uint32_t four = *reinterpret_cast<const uint32_t*>(scale + j * kMxTileBytes);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t e = 16 * i + sub;
-                    if (at + e < cols) row[at + e] = mx_round<T>(mx_decode1(in[e >> 1] >> (4 * (e & 1u)) & 15u) * mx_scale(four >> (8 * (i >> 1)) & 255u));
-                }
+        for (int j = 0; j < STRIP * (int)kTurns; ++j) {
+            const uint32_t at = from + j * 16 * kPer;
+            if (at < cols) {
+                w[j] = __ldcs(in + (at >> 3));
+                s[j] = scale_at(at >> 5);
+                if (!WIDE) {
+                    const uint32_t next = (at >> 3) + 1, last = min(at + kPer - 1, cols - 1);
+                    w[j] = __funnelshift_r(w[j], next < blocks * 4 ? in[next] : 0u, 4 * (at & 7u));
+                    s2[j] = last >> 5 == at >> 5 ? s[j] : scale_at(last >> 5);
+                } else if (kPer == 4) w[j] >>= 4 * (at & 7u);
             }
         }
+#pragma unroll
+        for (int j = 0; j < STRIP * (int)kTurns; ++j) {
+            const uint32_t at = from + j * 16 * kPer;
+            if (at >= cols) break;
+            float v[8];
+            if constexpr (kPer == 8) mx_decode8(w[j], v);
+            else {
+                // with half of its results unused, mx_decode8's unpacking came out wrong (the other half's) from this compiler
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[q] = mx_decode1(w[j] >> (4 * q) & 15u);
+            }
+            const float first = mx_scale(s[j]), second = WIDE ? first : mx_scale(s2[j]);
+            MxPack<T> p;
+#pragma unroll
+            for (int q = 0; q < (int)kPer; ++q) p.v[q] = mx_round<T>(v[q] * (WIDE || (at & 31u) + q < 32u ? first : second));
+            if (at + kPer <= cols) *reinterpret_cast<uint4*>(row + at) = *reinterpret_cast<const uint4*>(&p);
+            else {
+#pragma unroll
+                for (int q = 0; q < (int)kPer; ++q)
+                    if (at + q < cols) row[at + q] = p.v[q];
+            }
+        }
+        if (!WIDE && strip == 0 && sub < min(head, cols)) row[sub] = mx_round<T>(mx_decode1(in[0] >> (4 * sub) & 15u) * mx_scale(scale_at(0)));
         r += step_row;
         strip += step_strip;
         if (strip >= strips) { strip -= strips; ++r; }
@@ -377,7 +377,7 @@ unsigned plan(const zccl_mx4_job& j, size_t element, MxJob& to)
     }
     if (mx_bands(j.rows) * kMxBand * groups > kMxMaxGroups) return 0u;
     to.kind = at % 16 || j.pitch * element % 16 ? kMxRowsPlain : strips_pay(j.rows, groups) ? kMxRowsStrips : kMxRows;
-    const Rounds k = rounds_of(j.rows, groups, to.kind == kMxRowsStrips ? 4 : 1);
+    const Rounds k = rounds_of(j.rows, groups, to.kind == kMxRows ? 1 : 4);
     to.strips = k.strips;
     to.total = k.total;
     to.work = k.ctas;

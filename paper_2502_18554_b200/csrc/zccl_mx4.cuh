@@ -69,7 +69,8 @@ __device__ __forceinline__ float mx_decode1(uint32_t code)
     // E2M1 moved to binary32's exponent and mantissa is the value times 2^-126, its subnormal number one of binary32's
     return __uint_as_float(m << 22 | (code & 8u) << 28) * 0x1p126f;
 }
-__device__ __forceinline__ void mx_decode8(uint32_t w, float scale, float (&v)[8])
+// Eight codes as the numbers that E2M1 gives them (without the block's scale).
+__device__ __forceinline__ void mx_decode8(uint32_t w, float (&v)[8])
 {
     uint32_t h[4];
     asm("{\n\t.reg .b8 a, b, c, d;\n\t"
@@ -82,8 +83,8 @@ __device__ __forceinline__ void mx_decode8(uint32_t w, float scale, float (&v)[8
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-        v[2 * i] = f.x * scale;
-        v[2 * i + 1] = f.y * scale;
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
     }
 }
 
