@@ -606,27 +606,49 @@ PyObject* mx4_linear_backward(PyObject*, Args a, Py_ssize_t na)
 }
 
 // Entry i of a list that belongs to `like`: contiguous, of type `dt`, `n` elements, on the same device.
-bool entry(const Tensors& list, size_t i, c10::ScalarType dt, size_t n, const at::Tensor& like, const at::Tensor** t)
+bool refuse_entry(const Tensors& list, size_t i, c10::ScalarType dt, size_t n, const at::Tensor& like)
 {
-    if (!list.at(i, t)) return false;
-    if (!(*t)->is_contiguous() || (*t)->scalar_type() != dt || (size_t)(*t)->numel() != n) {
-        PyErr_Format(PyExc_ValueError, "tensor %zu of a list: expected %zu contiguous elements of %S", i, n, (PyObject*)torch::getTHPDtype(dt));
-        return false;
+    const at::Tensor* t;
+    if (!list.at(i, &t)) return false;
+    if (t->device() != like.device()) return refuse("all tensors of a call are on one device");
+    PyErr_Format(PyExc_ValueError, "tensor %zu of a list: expected %zu contiguous elements of %S", i, n, (PyObject*)torch::getTHPDtype(dt));
+    return false;
+}
+inline bool entry(const Tensors& list, size_t i, c10::ScalarType dt, size_t n, const at::Tensor& like, const at::Tensor** t)
+{
+    PyObject* const o = PySequence_Fast_GET_ITEM(list.seq, (Py_ssize_t)i);
+    if (THPVariable_Check(o)) {
+        const at::Tensor& x = THPVariable_Unpack(o);
+        if (x.scalar_type() == dt && (size_t)x.numel() == n && x.is_contiguous() && x.device() == like.device()) {
+            *t = &x;
+            return true;
+        }
     }
-    return (*t)->device() == like.device() || refuse("all tensors of a call are on one device");
+    return refuse_entry(list, i, dt, n, like);
 }
-// Whether no two of these ranges share a byte.
-bool apart(std::vector<std::pair<uintptr_t, uintptr_t>>& ranges)
-{
-    const auto clash = [&] {
+// Whether the tensors of a list share no byte.  Lists are in the order of memory more often than not: only others are sorted.
+struct Apart {
+    uintptr_t end = 0;
+    bool ordered = true;
+    void add(const void* p, size_t bytes)
+    {
+        ordered &= bytes == 0 || (uintptr_t)p >= end;
+        if (bytes) end = (uintptr_t)p + bytes;
+    }
+    // `at(i)` and `bytes(i)`: where tensor i is and how long
+    template <class F, class G>
+    bool ok(size_t count, F&& at, G&& bytes) const
+    {
+        if (ordered) return true;
+        std::vector<std::pair<uintptr_t, uintptr_t>> ranges;
+        for (size_t i = 0; i < count; ++i)
+            if (bytes(i)) ranges.emplace_back((uintptr_t)at(i), (uintptr_t)at(i) + bytes(i));
+        std::sort(ranges.begin(), ranges.end());
         for (size_t i = 1; i < ranges.size(); ++i)
-            if (ranges[i].first < ranges[i - 1].second) return true;
-        return false;
-    };
-    if (!clash()) return true;
-    std::sort(ranges.begin(), ranges.end());
-    return !clash();
-}
+            if (ranges[i].first < ranges[i - 1].second) return false;
+        return true;
+    }
+};
 
 // (params, grads, m, v, m_scales, v_scales, copies, lr, beta1, beta2, eps, weight_decay, step, seed, norm, max_norm, stream)
 // m_scales, v_scales, copies, norm: or None; lr: a number or a float32 tensor; step: a number or an int64 tensor
@@ -655,41 +677,44 @@ PyObject* adamw(PyObject*, Args a, Py_ssize_t na)
     if (copied && (k.param_type != ZCCL_F32 || k.copy_type == ZCCL_F32)) return refuse("copies are bfloat16 or float16 ones of float32 parameters"), nullptr;
     const c10::ScalarType pt = first->scalar_type(), gt = grad->scalar_type(), state = eight ? c10::ScalarType::Float8_e4m3fn : c10::kFloat;
     std::vector<zccl_adamw_tensor> list(count);
-    std::vector<const at::Tensor*> written;
-    std::vector<std::pair<uintptr_t, uintptr_t>> ranges[6];
-    written.reserve(6 * count);
-    const auto put = [&](int kind, const at::Tensor* x) {
-        written.push_back(x);
-        const uintptr_t at = (uintptr_t)x->data_ptr();
-        if (x->numel()) ranges[kind].emplace_back(at, at + (uintptr_t)x->nbytes());
-        return x->data_ptr();
-    };
+    Apart apart[6];
+    const size_t wide = c10::elementSize(pt), state_bytes = c10::elementSize(state);
     for (size_t i = 0; i < count; ++i) {
         zccl_adamw_tensor& s = list[i];
         if (!p.at(i, &t)) return nullptr;
         const size_t n = (size_t)t->numel(), blocks = (n + ZCCL_BLOCK - 1) / ZCCL_BLOCK;
         s.n = n;
         if (!entry(p, i, pt, n, *first, &t)) return nullptr;
-        s.p = put(0, t);
+        s.p = t->data_ptr();
         if (!entry(g, i, gt, n, *first, &t)) return nullptr;
         s.g = t->data_ptr();
         if (!entry(m, i, state, n, *first, &t)) return nullptr;
-        s.m = put(1, t);
+        s.m = t->data_ptr();
         if (!entry(v, i, state, n, *first, &t)) return nullptr;
-        s.v = put(2, t);
+        s.v = t->data_ptr();
         if (eight) {
             if (!entry(ms, i, c10::kByte, blocks, *first, &t)) return nullptr;
-            s.m_scale = put(3, t);
+            s.m_scale = t->data_ptr();
             if (!entry(vs, i, c10::kByte, blocks, *first, &t)) return nullptr;
-            s.v_scale = put(4, t);
+            s.v_scale = t->data_ptr();
+            apart[3].add(s.m_scale, blocks);
+            apart[4].add(s.v_scale, blocks);
         }
         if (copied) {
             if (!entry(copies, i, copy->scalar_type(), n, *first, &t)) return nullptr;
-            s.copy = put(5, t);
+            s.copy = t->data_ptr();
+            apart[5].add(s.copy, 2 * n);
         }
+        apart[0].add(s.p, n * wide);
+        apart[1].add(s.m, n * state_bytes);
+        apart[2].add(s.v, n * state_bytes);
     }
-    for (auto& r : ranges)
-        if (!apart(r)) return refuse("two tensors of a list overlap"), nullptr;
+    const auto blocks = [&](size_t i) { return (list[i].n + ZCCL_BLOCK - 1) / ZCCL_BLOCK; };
+    const auto states = [&](size_t i) { return list[i].n * state_bytes; };
+    if (!apart[0].ok(count, [&](size_t i) { return list[i].p; }, [&](size_t i) { return list[i].n * wide; }) || !apart[1].ok(count, [&](size_t i) { return list[i].m; }, states) ||
+        !apart[2].ok(count, [&](size_t i) { return list[i].v; }, states) || !apart[3].ok(count, [&](size_t i) { return list[i].m_scale; }, blocks) ||
+        !apart[4].ok(count, [&](size_t i) { return list[i].v_scale; }, blocks) || !apart[5].ok(count, [&](size_t i) { return list[i].copy; }, [&](size_t i) { return 2 * list[i].n; }))
+        return refuse("two tensors of a list overlap"), nullptr;
     const auto scalar = [&](PyObject* o, c10::ScalarType dt, const at::Tensor** x) {
         if (!cuda_tensor(o, x)) return false;
         if ((*x)->numel() != 1 || (*x)->scalar_type() != dt || (*x)->device() != first->device()) {
@@ -719,8 +744,13 @@ PyObject* adamw(PyObject*, Args a, Py_ssize_t na)
     void* st;
     if (PyErr_Occurred() || !stream_on(a[16], *first, &st)) return nullptr;
     PyObject* rc = status_on(*first, [&] { return zccl_adamw(list.data(), count, &k, st); });
-    for (const at::Tensor* x : written)
-        if (!x->is_inference()) x->unsafeGetTensorImpl()->bump_version();
+    // parameters and copies may have been saved for a backward pass
+    for (size_t i = 0; i < count; ++i)
+        for (const Tensors* l : {&p, copied ? &copies : nullptr})
+            if (l) {
+                const at::Tensor& x = THPVariable_Unpack(PySequence_Fast_GET_ITEM(l->seq, (Py_ssize_t)i));
+                if (!x.is_inference()) x.unsafeGetTensorImpl()->bump_version();
+            }
     return rc;
 }
 
