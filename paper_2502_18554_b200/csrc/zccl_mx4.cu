@@ -244,7 +244,7 @@ __device__ __forceinline__ void quantize_one(const MxJob& job, uint32_t cta, Col
 // spilled registers buy: whole pairs of 16-bit elements four (8192 x 8192 bf16: 26.7 us; three 28.1, two 34.1), the others three (16384 x 4097 bf16:
 // 45.9 us; four 63.3, two 55.5).
 template <class T, MxKind KIND>
-__global__ void __launch_bounds__(kMxThreads, KIND < kMxColumns ? 1 : KIND == kMxColumns && sizeof(T) == 2 ? 4 : 3) mx_quantize_kernel(const __grid_constant__ MxJob job)
+__global__ void __launch_bounds__(kMxThreads, KIND < kMxColumns ? (sizeof(T) == 2 ? 6 : 4) : KIND == kMxColumns && sizeof(T) == 2 ? 4 : 3) mx_quantize_kernel(const __grid_constant__ MxJob job)
 {
     __shared__ ColumnsShared sh;
     pdl_enter();

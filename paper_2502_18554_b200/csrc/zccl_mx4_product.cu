@@ -152,7 +152,7 @@ __device__ __forceinline__ void store_columns_any(const Product& k, unsigned cha
 // pieces out of each other's shared memory, each CTA some of the columns (or rows), so there is no workspace and no order that changes.
 // Bound by latency, or for weights that do not stay in L2 by memory.  The few rows go along the instruction's columns (16 at least), the many along
 // its 128 lanes: a stage is then little else than the weights.  More than one CTA to an SM: none allocates more tensor memory than its
-// share by shared memory (kSplitColumns), or clusters could wait for each other's.
+// share by shared memory (SplitShape::kColumns), or clusters could wait for each other's.
 template <int BN>
 struct SplitShape {
     static constexpr int kStages = BN == 128 ? 3 : 4;
@@ -359,35 +359,32 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
 
 // ---------------------------------------------------------------- many tiles
 
-// A pair of CTAs (the two of a cluster) works on a tile of 256 x BN: the first issues instructions that use both tensor cores, each CTA brings and
-// keeps its 128 rows of one operand and half of the other, so an SM reads 128 + BN / 2 rows for 128 x BN sums.  What bounds it is the
-// way from L2 to shared memory: with tiles of 128 x 192 to a single CTA the large product took 157 us (4096 x 8192 x 8192), 12 TB/s.
-// Eight warps read a tile's sums out, each half of the columns of a quarter of the rows, all into registers at once: sums of 256 columns do not fit tensor
-// memory twice next to the scales, so the next tile's instructions wait for that (of 128 columns there are two sets).
-constexpr int kPairWarps = 8, kPairThreads = 64 + 32 * kPairWarps;
-template <int BN>
+// A pair of CTAs (the two of a cluster) works on a tile of 256 x 256: the first issues instructions that use both tensor cores, each CTA brings and
+// keeps its 128 rows of one operand and half of the other, so an SM reads 256 rows for 128 x 256 sums.  (Tiles of 128 x 192 to a single CTA were bound by
+// the way from L2: 157 us for 4096 x 8192 x 8192, 12 TB/s; so are narrower tiles of a pair, whose stages take nearly as long.)  Now 100 us, 5.5 PFLOP/s, the
+// tensor cores active for 70 % of the cycles: what is left goes by how fast the one thread issues and by the power that the clock is given.
+// Eight warps read a tile's sums out, each half of the columns of a quarter of the rows, all into registers at once: 256 columns of sums do not fit tensor
+// memory twice next to the scales, so the next tile's instructions wait for that.
 struct PairShape {
-    static constexpr int kStages = BN == 256 ? 5 : 7;
-    static constexpr int kBands = BN / kMxBand;                                  // tiles of scales that a tile's columns lie in
-    static constexpr int kColAt = kRows * kRowBytes, kRowScaleAt = kColAt + BN / 2 * kRowBytes, kColScaleAt = kRowScaleAt + 2 * kMxTileBytes;
+    static constexpr int kCols = 256, kStages = 5;
+    static constexpr int kBands = kCols / kMxBand;                               // tiles of scales that a tile's columns lie in
+    static constexpr int kColAt = kRows * kRowBytes, kRowScaleAt = kColAt + kCols / 2 * kRowBytes, kColScaleAt = kRowScaleAt + 2 * kMxTileBytes;
     static constexpr int kStage = kColScaleAt + 2 * kMxTileBytes * kBands;
     static constexpr int kScaleColumns = 8 + 8 * kBands;                         // of tensor memory, a set for each stage
-    static constexpr int kSums = BN == 256 ? 1 : 2;
-    static constexpr int kScaleAt = kSums * BN;
     static constexpr int kColumns = 512;
-    static constexpr size_t kBytes = (size_t)kStage * kStages + kPairWarps * 32 * kOutPitch + 1024;
-    static_assert(kScaleAt + kStages * kScaleColumns <= kColumns, "tensor memory");
+    static constexpr int kWarps = 8, kThreads = 64 + 32 * kWarps;                // that read sums out, and all
+    static constexpr size_t kBytes = (size_t)kStage * kStages + kWarps * 32 * kOutPitch + 1024;
+    static_assert(kCols + kStages * kScaleColumns <= kColumns, "tensor memory");
     static_assert(kBytes <= 227 * 1024 && kBytes > 114 * 1024, "one CTA to an SM");
 };
 
-template <int BN>
-__global__ void __launch_bounds__(kPairThreads, 1) mx4_pair_kernel(const __grid_constant__ CUtensorMap r_map, const __grid_constant__ CUtensorMap c_map, const __grid_constant__ CUtensorMap r_scale_map,
+__global__ void __launch_bounds__(PairShape::kThreads, 1) mx4_pair_kernel(const __grid_constant__ CUtensorMap r_map, const __grid_constant__ CUtensorMap c_map, const __grid_constant__ CUtensorMap r_scale_map,
                                                                       const __grid_constant__ CUtensorMap c_scale_map, const __grid_constant__ Product k)
 {
-    using S = PairShape<BN>;
-    constexpr int kStages = S::kStages;
+    using S = PairShape;
+    constexpr int kStages = S::kStages, BN = S::kCols;
     extern __shared__ unsigned char raw[];
-    __shared__ unsigned long long full[kStages], empty[kStages], done[2], free_[2], drained;
+    __shared__ unsigned long long full[kStages], empty[kStages], done, free_, drained;
     __shared__ uint32_t tmem_at;
     unsigned char* const tiles = on_1024(raw);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, rank = cluster_rank();
@@ -401,10 +398,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx4_pair_kernel(const __grid_
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], 1);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(&done[i], 1);
-            mbar_init(&free_[i], 2 * kPairWarps);
-        }
+        mbar_init(&done, 1);
+        mbar_init(&free_, 2 * S::kWarps);
         mbar_init(&drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -450,8 +445,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx4_pair_kernel(const __grid_
             // What bounds a large product is how fast this thread issues: a stage's instructions run for 512 cycles, and with one wait more to a stage (or the
             // next stage's scales in front of this one's instructions) 4096 x 8192 x 8192 took 20 to 30 us longer.
             const uint32_t base = smem_u32(tiles);
-            const auto issue = [&](uint32_t s, uint32_t sums, bool add, uint32_t groups, uint32_t steps) {
-                const uint32_t at = base + s * S::kStage, r_scale = tmem + S::kScaleAt + s * S::kScaleColumns, c_scale = r_scale + 8;
+            const auto issue = [&](uint32_t s, bool add, uint32_t groups, uint32_t steps) {
+                const uint32_t at = base + s * S::kStage, r_scale = tmem + BN + s * S::kScaleColumns, c_scale = r_scale + 8;
                 const unsigned long long r_codes = operand_descriptor(at), c_codes = operand_descriptor(at + S::kColAt), r_in = scales_descriptor(at + S::kRowScaleAt),
                                          c_in = scales_descriptor(at + S::kColScaleAt);
 #pragma unroll
@@ -464,29 +459,28 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx4_pair_kernel(const __grid_
 #pragma unroll
                 for (uint32_t j = 0; j < 4; ++j)
                     if (j < steps)
-                        tcgen05_mma_mx4_pair(sums, r_codes + 2 * j, c_codes + 2 * j, mx4_instruction(2 * kRows, BN, (j & 1) * 2), r_scale + 4 * (j / 2),
+                        tcgen05_mma_mx4_pair(tmem, r_codes + 2 * j, c_codes + 2 * j, mx4_instruction(2 * kRows, BN, (j & 1) * 2), r_scale + 4 * (j / 2),
                                              c_scale + 4 * S::kBands * (j / 2), add || j > 0);
             };
             uint32_t s = 0, parity = 0, i = 0;
             bool ok = true;
             for (uint32_t t = first; t < total && ok; t += stride, ++i) {
-                const uint32_t b = i % S::kSums, sums = tmem + b * BN;
-                if (i >= S::kSums) {
-                    if (!(ok = wait_for_cluster(&free_[b], (i / S::kSums - 1) & 1))) break;
+                if (i >= 1) {
+                    if (!(ok = wait_for_cluster(&free_, (i - 1) & 1))) break;
                     tcgen05_fence_after();
                 }
                 for (uint32_t d = 0; d < depth_tiles; ++d) {
                     if (!(ok = wait_for(&full[s], parity))) break;
                     tcgen05_fence_after();
-                    if (d + 1 < depth_tiles) issue(s, sums, d > 0, 2, 4);
-                    else issue(s, sums, d > 0, groups_at(d, k.depth_blocks), steps_at(d, k.depth_blocks));
+                    if (d + 1 < depth_tiles) issue(s, d > 0, 2, 4);
+                    else issue(s, d > 0, groups_at(d, k.depth_blocks), steps_at(d, k.depth_blocks));
                     tcgen05_commit_pair(&empty[s]);
                     if (++s == kStages) {
                         s = 0;
                         parity ^= 1;
                     }
                 }
-                tcgen05_commit_pair(&done[b]);
+                tcgen05_commit_pair(&done);
             }
             tcgen05_commit_pair(&drained);
             wait_for(&drained, 0);
@@ -498,12 +492,12 @@ __global__ void __launch_bounds__(kPairThreads, 1) mx4_pair_kernel(const __grid_
         for (uint32_t t = first; t < total; t += stride, ++i) {
             uint32_t rt, ct;
             tile_of(k, t, kBand, rt, ct);
-            const uint32_t b = i % S::kSums, c = half * (BN / 2);
-            if (!wait_for(&done[b], (i / S::kSums) & 1)) break;
+            const uint32_t c = half * (BN / 2);
+            if (!wait_for(&done, i & 1)) break;
             tcgen05_fence_after();
-            store_columns_any<BN / 2>(k, out, tmem + b * BN + c + (quarter * 32 << 16), (rt * 2 + rank) * kRows + quarter * 32, ct * BN + c, [&] {
+            store_columns_any<BN / 2>(k, out, tmem + c + (quarter * 32 << 16), (rt * 2 + rank) * kRows + quarter * 32, ct * BN + c, [&] {
                 __syncwarp();
-                if (lane == 0) mbar_arrive_at(&free_[b], 0);
+                if (lane == 0) mbar_arrive_at(&free_, 0);
             });
         }
     }
@@ -527,8 +521,6 @@ ProductDevice g_product_dev[kMaxDevices];
 
 template <int BN>
 cudaError_t split_attr() { return cudaFuncSetAttribute(mx4_split_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SplitShape<BN>::kBytes); }
-template <int BN>
-cudaError_t pair_attr() { return cudaFuncSetAttribute(mx4_pair_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairShape<BN>::kBytes); }
 
 cudaError_t product_device(const ProductDevice** out)
 {
@@ -552,19 +544,18 @@ cudaError_t product_device(const ProductDevice** out)
         if (e == cudaSuccess) e = split_attr<32>();
         if (e == cudaSuccess) e = split_attr<64>();
         if (e == cudaSuccess) e = split_attr<128>();
-        if (e == cudaSuccess) e = pair_attr<128>();
-        if (e == cudaSuccess) e = pair_attr<256>();
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(mx4_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairShape::kBytes);
         if (e != cudaSuccess) return e;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)d.sms / 2 * 2);
-        cfg.blockDim = dim3(kPairThreads);
-        cfg.dynamicSmemBytes = PairShape<256>::kBytes;
+        cfg.blockDim = dim3(PairShape::kThreads);
+        cfg.dynamicSmemBytes = PairShape::kBytes;
         cudaLaunchAttribute attr;
         attr.id = cudaLaunchAttributeClusterDimension;
         attr.val.clusterDim.x = 2; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
-        e = cudaOccupancyMaxActiveClusters(&d.pairs, mx4_pair_kernel<256>, &cfg);
+        e = cudaOccupancyMaxActiveClusters(&d.pairs, mx4_pair_kernel, &cfg);
         if (e != cudaSuccess) return e;
         if (d.pairs < 1) return cudaErrorNotSupported;
         d.ready = true;
@@ -616,15 +607,14 @@ int launch_split(const Sides& s, Product k, unsigned parts, cudaStream_t st)
     if (!operand_map(&r, s.r_codes, s.rows, k.depth_blocks, kRows) || !operand_map(&c, s.c_codes, s.cols, k.depth_blocks, BN)) return ZCCL_E_CUDA;
     return launched(launch_cluster(parts, mx4_split_kernel<BN>, dim3(k.row_tiles * k.col_tiles * parts), dim3(kProductThreads), SplitShape<BN>::kBytes, st, r, c, k));
 }
-template <int BN>
 int launch_pair(const Sides& s, Product k, int pairs, cudaStream_t st)
 {
     CUtensorMap r, c, rs, cs;
-    if (!set_tiles(k, s, 2 * kRows, BN)) return ZCCL_E_ARG;
-    if (!operand_map(&r, s.r_codes, s.rows, k.depth_blocks, kRows) || !operand_map(&c, s.c_codes, s.cols, k.depth_blocks, BN / 2) ||
-        !scales_map(&rs, k.r_scales, s.rows, k.depth_blocks, 1) || !scales_map(&cs, k.c_scales, s.cols, k.depth_blocks, PairShape<BN>::kBands)) return ZCCL_E_CUDA;
+    if (!set_tiles(k, s, 2 * kRows, PairShape::kCols)) return ZCCL_E_ARG;
+    if (!operand_map(&r, s.r_codes, s.rows, k.depth_blocks, kRows) || !operand_map(&c, s.c_codes, s.cols, k.depth_blocks, PairShape::kCols / 2) ||
+        !scales_map(&rs, k.r_scales, s.rows, k.depth_blocks, 1) || !scales_map(&cs, k.c_scales, s.cols, k.depth_blocks, PairShape::kBands)) return ZCCL_E_CUDA;
     const unsigned clusters = std::min(k.row_tiles * k.col_tiles, (unsigned)pairs);
-    return launched(launch_cluster(2, mx4_pair_kernel<BN>, dim3(2 * clusters), dim3(kPairThreads), PairShape<BN>::kBytes, st, r, c, rs, cs, k));
+    return launched(launch_cluster(2, mx4_pair_kernel, dim3(2 * clusters), dim3(PairShape::kThreads), PairShape::kBytes, st, r, c, rs, cs, k));
 }
 
 bool aligned16(const void* p) { return p && ((uintptr_t)p & 15u) == 0; }
@@ -680,10 +670,7 @@ int multiply(const void* a_codes, const void* a_scales, size_t m, const void* b_
         if (sides.cols <= 64) return launch_split<64>(sides, p, parts, st);
         return launch_split<128>(sides, p, parts, st);
     }
-    // whichever is through in less: a round of tiles half as wide takes a little more than half as long
-    const size_t pairs = (size_t)dev->pairs, rounds_256 = up(up(sides.rows, 256) * up(sides.cols, 256), pairs), rounds_128 = up(up(sides.rows, 256) * up(sides.cols, 128), pairs);
-    if (rounds_256 <= rounds_128) return launch_pair<256>(sides, p, dev->pairs, st);
-    return launch_pair<128>(sides, p, dev->pairs, st);
+    return launch_pair(sides, p, dev->pairs, st);
 }
 
 }  // namespace

@@ -2,8 +2,6 @@
 #include "../../include/zccl.h"
 #include "zccl_mx4.cuh"
 
-#include <cuda_fp8.h>
-
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -47,11 +45,32 @@ __device__ __forceinline__ Eight<T> load_wide(const T* p)
     for (int i = 0; i < (int)sizeof(T) / 2; ++i) e.w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
     return e;
 }
-template <class T>
-__device__ __forceinline__ void values_of(const Eight<T>& e, float (&v)[8])
+__device__ __forceinline__ void values_of(const Eight<float>& e, float (&v)[8])
 {
+    const uint32_t w[8] = {e.w[0].x, e.w[0].y, e.w[0].z, e.w[0].w, e.w[1].x, e.w[1].y, e.w[1].z, e.w[1].w};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = mx_float(reinterpret_cast<const T*>(e.w)[i]);
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+}
+__device__ __forceinline__ void values_of(const Eight<__nv_bfloat16>& e, float (&v)[8])
+{
+    const uint32_t w[4] = {e.w[0].x, e.w[0].y, e.w[0].z, e.w[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void two_halves(uint32_t w, float& a, float& b)
+{
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    a = f.x;
+    b = f.y;
+}
+__device__ __forceinline__ void values_of(const Eight<__half>& e, float (&v)[8])
+{
+    const uint32_t w[4] = {e.w[0].x, e.w[0].y, e.w[0].z, e.w[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) two_halves(w[i], v[2 * i], v[2 * i + 1]);
 }
 __device__ __forceinline__ uint32_t two_of(float a, float b, __nv_bfloat16)
 {
@@ -251,12 +270,11 @@ __device__ __forceinline__ uint32_t exponent8(uint32_t top)
 __device__ __forceinline__ void decode8(uint2 w, float (&v)[8])
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t two = (i & 2 ? w.y : w.x) >> (16 * (i & 1));
-        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(two & 0xFFFFu), __NV_E4M3);
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-        v[2 * i] = f.x;
-        v[2 * i + 1] = f.y;
+    for (int i = 0; i < 2; ++i) {
+        uint32_t a, b;
+        asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(a), "=r"(b) : "r"(i ? w.y : w.x));
+        two_halves(a, v[4 * i], v[4 * i + 1]);
+        two_halves(b, v[4 * i + 2], v[4 * i + 3]);
     }
 }
 __device__ __forceinline__ uint2 read_codes(const unsigned char* p, bool full, int left)
