@@ -451,9 +451,10 @@ int zccl_mx4_matmul(const void* a_codes, const void* a_scales, size_t m, const v
                     void* y, int type, size_t pitch, void* stream);
 int zccl_mx4_status(void* stream);
 /*
- * A layer with weights in this form, y [m x n] <- Q(x) W^T in x's type: zccl_mx4_quantize of x [m x k, `x_pitch`] along its rows into x_codes and
- * x_scales (room for the form of an m x k matrix; for calls that may run at the same time, each its own), then zccl_mx4_matmul, which for few rows begins
- * to bring the weights while x is still quantised.
+ * A layer with weights in this form, y [m x n] <- Q(x) W^T in x's type (x [m x k, `x_pitch`]): the bits of zccl_mx4_quantize of x along its rows and
+ * zccl_mx4_matmul.  x_codes and x_scales are room for the form of an m x k matrix; calls that may run at the same time need one each.  A few rows are
+ * quantised inside the product (one launch; what is in x_codes and x_scales afterwards is unspecified), else the product of few rows begins to bring the weights
+ * while x is still quantised.
  */
 int zccl_mx4_linear(const void* x, int type, size_t m, size_t k, size_t x_pitch, const void* w_codes, const void* w_scales, size_t n,
                     void* x_codes, void* x_scales, void* y, size_t pitch, void* stream);

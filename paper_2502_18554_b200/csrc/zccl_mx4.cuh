@@ -62,6 +62,70 @@ __device__ __forceinline__ uint32_t mx_encode8(const float (&v)[8])
         : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
     return w;
 }
+// Two elements of a 16-bit type in a word, or of binary32 in two.
+template <class T> struct MxTwo { uint32_t w; };
+template <> struct MxTwo<float> { float a, b; };
+
+// Largest magnitudes so far of the two places, as bits: magnitudes of floats are in the order of their bits, with infinity and
+// NaN at the top, so 16-bit types are compared as two halves of a word.
+template <class T> struct MxTop { uint32_t w = 0; };
+template <> struct MxTop<float> { uint32_t a = 0, b = 0; };
+template <class T>
+__device__ __forceinline__ void mx_top(MxTop<T>& top, const MxTwo<T>& v) { top.w = __vmaxu2(top.w, v.w & 0x7FFF7FFFu); }
+__device__ __forceinline__ void mx_top(MxTop<float>& top, const MxTwo<float>& v)
+{
+    top.a = max(top.a, __float_as_uint(v.a) & 0x7FFFFFFFu);
+    top.b = max(top.b, __float_as_uint(v.b) & 0x7FFFFFFFu);
+}
+// The bits of a magnitude in binary32.
+template <class T> __device__ __forceinline__ uint32_t mx_bits(uint32_t half);
+template <> __device__ __forceinline__ uint32_t mx_bits<__nv_bfloat16>(uint32_t half) { return half << 16; }
+template <> __device__ __forceinline__ uint32_t mx_bits<__half>(uint32_t half) { return __float_as_uint(__half2float(__ushort_as_half((unsigned short)half))); }
+template <class T> __device__ __forceinline__ uint32_t mx_first(const MxTop<T>& top) { return mx_bits<T>(top.w & 0xFFFFu); }
+template <class T> __device__ __forceinline__ uint32_t mx_second(const MxTop<T>& top) { return mx_bits<T>(top.w >> 16); }
+__device__ __forceinline__ uint32_t mx_first(const MxTop<float>& top) { return top.a; }
+__device__ __forceinline__ uint32_t mx_second(const MxTop<float>& top) { return top.b; }
+
+// Both elements times their powers of two, exactly, as binary32.  bfloat16 has binary32's exponents, so there the product of two elements is
+// one instruction (what falls below its range is far below the smallest code's half).
+template <class T>
+__device__ __forceinline__ void mx_scaled(const MxTwo<T>& v, float first, float second, uint32_t, float& a, float& b)
+{
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v.w));
+    a = f.x * first;
+    b = f.y * second;
+}
+__device__ __forceinline__ void mx_scaled(const MxTwo<float>& v, float first, float second, uint32_t, float& a, float& b)
+{
+    a = v.a * first;
+    b = v.b * second;
+}
+__device__ __forceinline__ void mx_scaled(const MxTwo<__nv_bfloat16>& v, float, float, uint32_t both, float& a, float& b)
+{
+    const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&v.w), *reinterpret_cast<const __nv_bfloat162*>(&both));
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(&p);
+    a = __uint_as_float(w << 16);
+    b = __uint_as_float(w & 0xFFFF0000u);
+}
+// 2^-e of two places as a pair of bfloat16.
+__device__ __forceinline__ uint32_t mx_pair(float first, float second) { return __float_as_uint(first) >> 16 | (__float_as_uint(second) & 0xFFFF0000u); }
+
+// Eight neighbouring elements of a row; what lies behind `cols` counts as zero.
+template <class T, bool VEC>
+__device__ __forceinline__ void load8(const T* __restrict__ row, uint32_t at, uint32_t cols, MxTwo<T> (&v)[4])
+{
+    if (VEC && at + 8 <= cols) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(v)[i] = __ldcs(reinterpret_cast<const uint4*>(row + at) + i);
+    } else {
+        T e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = at + i < cols ? row[at + i] : mx_round<T>(0.0f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const MxTwo<T>*>(&e[2 * i]);
+    }
+}
+
 // One code (four bits): magnitudes 0 ... 3 are halves of their index, 4 ... 7 have two mantissas to a binade.
 __device__ __forceinline__ float mx_decode1(uint32_t code)
 {
@@ -86,6 +150,28 @@ __device__ __forceinline__ void mx_decode8(uint32_t w, float (&v)[8])
         v[2 * i] = f.x;
         v[2 * i + 1] = f.y;
     }
+}
+
+// Sixteen lanes' run of 128 elements, eight to a lane: the lane's codes, and in `four` the run's four biased exponents as a word (every lane's).
+template <class T>
+__device__ __forceinline__ uint32_t quantize_run(const MxTwo<T> (&v)[4], uint32_t sub, uint32_t& four)
+{
+    MxTop<T> two;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mx_top(two, v[i]);
+    uint32_t top = max(mx_first(two), mx_second(two));
+    top = max(top, __shfl_xor_sync(kFull, top, 1));
+    top = max(top, __shfl_xor_sync(kFull, top, 2));
+    const uint32_t s = mx_exponent(top);
+    const float inverse = mx_inverse(s);
+    const uint32_t both = mx_pair(inverse, inverse);
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mx_scaled(v[i], inverse, inverse, both, f[2 * i], f[2 * i + 1]);
+    four = s << (8 * (sub >> 2));
+    four |= __shfl_xor_sync(kFull, four, 4);
+    four |= __shfl_xor_sync(kFull, four, 8);
+    return s == 255u ? 0u : mx_encode8(f);
 }
 
 }  // namespace

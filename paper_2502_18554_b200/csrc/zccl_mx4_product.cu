@@ -357,6 +357,163 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
     if (warp == 1) tmem_free(tmem, S::kColumns);
 }
 
+// ---------------------------------------------------------------- a few tokens
+
+// The layer of a few rows in one launch: mx4_split_kernel<16> across, whose CTAs quantise their piece of x themselves, into the places in shared memory
+// where a load would have put it, while the first weights are on their way.  A quantisation of its own takes 1.4 us and leaves the memory idle for
+// longer (1 x 8192 x 16384 with weights from memory: 17.2 us as two launches).  Every CTA quantises all of its piece, so there may not be much of it (kMostUnits).
+struct TokenShape {
+    using S = SplitShape<16>;
+    static constexpr int kStages = S::kStages, kRowScaleAt = kRows * kRowBytes, kStage = kRowScaleAt + 2 * kMxTileBytes;
+    // a depth tile of x: 16 rows of codes, and two tiles of scales of which 16 rows count; the rest of a tile is the next one's, or nothing
+    static constexpr int kCodes = 16 * kRowBytes, kScales = 256;
+    static constexpr uint32_t kMostUnits = 128;                                  // runs of 128 elements of a row
+    static constexpr size_t kMostBytes = 112 * 1024;                             // two CTAs to an SM
+    static size_t bytes(size_t depth_tiles) { return (size_t)kStage * kStages + depth_tiles * (kCodes + 2 * kScales) + kMxTileBytes + 1024; }
+    static_assert(16 * kRows * 4 <= kStage * kStages, "sums take the stages' place");
+    static_assert(((228 * 1024) / (kStage * kStages + 1024)) * S::kColumns <= 512, "clusters must not wait for each other's tensor memory");
+};
+struct Tokens {
+    const void* x;
+    size_t pitch;
+    uint32_t cols;
+    int vec;                                  // every row of x begins on a 16-byte boundary
+};
+
+template <class T>
+__global__ void __launch_bounds__(kProductThreads, 1) mx4_token_kernel(const __grid_constant__ CUtensorMap r_map, const __grid_constant__ Product k, const __grid_constant__ Tokens x)
+{
+    using S = TokenShape;
+    constexpr int kStages = S::kStages, BN = 16;
+    extern __shared__ unsigned char raw[];
+    __shared__ unsigned long long full[kStages], empty[kStages], done;
+    __shared__ uint32_t tmem_at;
+    unsigned char* const tiles = on_1024(raw);
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+
+    if (warp == 0 && lane == 0) {
+        prefetch_map(&r_map);
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], 1);
+        }
+        mbar_init(&done, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(&tmem_at, S::S::kColumns);
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = tmem_at;
+    pdl_enter();
+
+    uint32_t parts;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
+    const uint32_t depth_tiles = (k.depth_blocks + 7) / 8, part = cluster_rank(), rt = blockIdx.x / parts;
+    const uint32_t k_begin = (uint32_t)((unsigned long long)depth_tiles * part / parts), k_end = (uint32_t)((unsigned long long)depth_tiles * (part + 1) / parts);
+    const uint32_t groups = (k.depth_blocks + 3) / 4, mine = k_end - k_begin;
+    unsigned char* const codes = tiles + S::kStage * kStages;
+    unsigned char* const scales = codes + (size_t)mine * S::kCodes;
+    const auto load = [&](uint32_t n) {
+        const uint32_t s = n % kStages, d = k_begin + n, scale_bytes = groups_at(d, k.depth_blocks) * kMxTileBytes;
+        unsigned char* const at = tiles + s * S::kStage;
+        mbar_expect_tx(&full[s], kRows * kRowBytes + scale_bytes);
+        tile_load(at, &r_map, (int)(d * kRowBytes), (int)(rt * kRows), &full[s]);
+        bytes_load(at + S::kRowScaleAt, k.r_scales + ((size_t)rt * groups + 2 * d) * kMxTileBytes, scale_bytes, &full[s]);
+    };
+    uint32_t asked = 0;
+    if (warp == 0 && lane == 0)
+        for (; asked < (uint32_t)kStages && asked < mine; ++asked) load(asked);
+    __syncwarp();
+
+    // x: 16 lanes take a run of 128 elements of a row, as in quantising to memory; four runs are loaded at a time
+    {
+        const uint32_t sub = threadIdx.x & 15u, g_begin = 2 * k_begin, runs = min(2 * k_end, groups) - g_begin, units = k.cols * runs;
+        constexpr uint32_t kHalves = kProductThreads / 16, kAtOnce = 4;
+        for (uint32_t u0 = (threadIdx.x >> 4) & ~1u; u0 < units; u0 += kHalves * kAtOnce) {
+            const uint32_t u = u0 + (lane >> 4);
+            MxTwo<T> v[kAtOnce][4];
+#pragma unroll
+            for (uint32_t i = 0; i < kAtOnce; ++i) {
+                const uint32_t at_u = u + i * kHalves, r = at_u / runs, at = (g_begin + at_u - r * runs) * kMxGroup + sub * 8;
+                if (at_u < units && at < x.cols) {
+                    const T* const row = (const T*)x.x + (size_t)r * x.pitch;
+                    if (x.vec) load8<T, true>(row, at, x.cols, v[i]);
+                    else load8<T, false>(row, at, x.cols, v[i]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[i][j] = MxTwo<T>{};
+                }
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < kAtOnce; ++i) {
+                uint32_t s;
+                const uint32_t w = quantize_run(v[i], sub, s), at_u = u + i * kHalves;
+                if (at_u < units) {
+                    const uint32_t r = at_u / runs, g = at_u - r * runs, piece = (g & 1u) * 4 + (sub >> 2);
+                    *reinterpret_cast<uint32_t*>(codes + (g >> 1) * S::kCodes + r * kRowBytes + ((piece ^ (r & 7u)) << 4) + (sub & 3u) * 4) = w;
+                    if (sub == 0) *reinterpret_cast<uint32_t*>(scales + g * S::kScales + r * 16) = s;
+                }
+            }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t n = asked;
+            for (; n < mine; ++n) {
+                if (n >= (uint32_t)kStages && !wait_for(&empty[n % kStages], (n / kStages - 1) & 1)) break;
+                load(n);
+            }
+            for (uint32_t i = n < (uint32_t)kStages ? 0 : n - kStages; i < n; ++i) wait_for(&full[i % kStages], (i / kStages) & 1);
+        }
+    } else if (warp == 1) {
+        if (elect_one()) {
+            for (uint32_t n = 0; n < mine; ++n) {
+                const uint32_t s = n % kStages, d = k_begin + n;
+                if (!wait_for(&full[s], (n / kStages) & 1)) break;
+                tcgen05_fence_after();
+                const uint32_t at = smem_u32(tiles) + s * S::kStage, r_scale = tmem + S::S::kSumColumns + s * S::S::kScaleColumns, c_scale = r_scale + 8;
+                for (uint32_t g = 0; g < groups_at(d, k.depth_blocks); ++g) {
+                    tcgen05_copy_scales(r_scale + 4 * g, scales_descriptor(at + S::kRowScaleAt + g * kMxTileBytes));
+                    tcgen05_copy_scales(c_scale + 4 * g, scales_descriptor(smem_u32(scales) + (2 * n + g) * S::kScales));
+                }
+                const unsigned long long r_codes = operand_descriptor(at), c_codes = operand_descriptor(smem_u32(codes) + n * S::kCodes);
+                const uint32_t steps = steps_at(d, k.depth_blocks);
+                for (uint32_t j = 0; j < steps; ++j)
+                    tcgen05_mma_mx4(tmem, r_codes + 2 * j, c_codes + 2 * j, mx4_instruction(kRows, BN, (j & 1) * 2), r_scale + 4 * (j / 2), c_scale + 4 * (j / 2), n > 0 || j > 0);
+                tcgen05_commit(&empty[s]);
+            }
+            tcgen05_commit(&done);
+            wait_for(&done, 0);
+        }
+    } else if (wait_for(&done, 0)) {
+        tcgen05_fence_after();
+        const uint32_t quarter = warp & 3u;
+        float* const to = reinterpret_cast<float*>(tiles) + quarter * 32 + lane;
+        uint32_t v[32];
+        tcgen05_load16(tmem + (quarter * 32 << 16), v);
+        tcgen05_wait_loads();
+#pragma unroll
+        for (int j = 0; j < BN; ++j) to[j * kRows] = __uint_as_float(v[j]);
+        tcgen05_fence_before();
+    }
+    __syncwarp();
+    cluster_sync();
+    if (warp >= 2) {
+        const uint32_t sums = smem_u32(tiles), r0 = rt * kRows;
+        if (parts == 8) store_share<BN, 8>(k, sums, part, r0, 0);
+        else if (parts == 4) store_share<BN, 4>(k, sums, part, r0, 0);
+        else if (parts == 2) store_share<BN, 2>(k, sums, part, r0, 0);
+        else store_share<BN, 1>(k, sums, part, r0, 0);
+    }
+    __syncwarp();
+    cluster_sync();                        // nobody leaves while its sums are still read
+    if (warp == 1) tmem_free(tmem, S::S::kColumns);
+}
+
 // ---------------------------------------------------------------- many tiles
 
 // A pair of CTAs (the two of a cluster) works on a tile of 256 x 256: the first issues instructions that use both tensor cores, each CTA brings and
@@ -522,6 +679,9 @@ ProductDevice g_product_dev[kMaxDevices];
 template <int BN>
 cudaError_t split_attr() { return cudaFuncSetAttribute(mx4_split_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SplitShape<BN>::kBytes); }
 
+template <class T>
+cudaError_t token_attr() { return cudaFuncSetAttribute(mx4_token_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TokenShape::kMostBytes); }
+
 cudaError_t product_device(const ProductDevice** out)
 {
     int dev = 0;
@@ -544,6 +704,9 @@ cudaError_t product_device(const ProductDevice** out)
         if (e == cudaSuccess) e = split_attr<32>();
         if (e == cudaSuccess) e = split_attr<64>();
         if (e == cudaSuccess) e = split_attr<128>();
+        if (e == cudaSuccess) e = token_attr<float>();
+        if (e == cudaSuccess) e = token_attr<__nv_bfloat16>();
+        if (e == cudaSuccess) e = token_attr<__half>();
         if (e == cudaSuccess) e = cudaFuncSetAttribute(mx4_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PairShape::kBytes);
         if (e != cudaSuccess) return e;
         cudaLaunchConfig_t cfg = {};
@@ -630,6 +793,33 @@ unsigned parts_of(size_t tiles, size_t depth_tiles, size_t sms, bool wide)
     return wide && depth_tiles - up(depth_tiles, parts) < 7 ? 1 : parts;
 }
 
+// The layer of a few tokens in one launch; false where that would not pay (see mx4_token_kernel) or the arguments are wrong.
+template <class T>
+bool tokens(const T* x, int type, size_t m, size_t k, size_t x_pitch, const void* w_codes, const void* w_scales, size_t n, void* y, size_t pitch, cudaStream_t st, int& rc)
+{
+    const ProductDevice* dev;
+    const size_t depth_tiles = up(k, kDepth), row_tiles = up(n, kRows);
+    if (m > 16 || m >= n || n > 0x7FFFFF00u || k > 0x7FFFFF00u || product_device(&dev) != cudaSuccess) return false;
+    const unsigned parts = parts_of(row_tiles, depth_tiles, (size_t)dev->sms, false);
+    const size_t mine = up(depth_tiles, parts), bytes = TokenShape::bytes(mine);
+    if (m * std::min(2 * mine, mx_groups(k)) > TokenShape::kMostUnits || bytes > TokenShape::kMostBytes || row_tiles * parts > 0x7FFFFFFFu) return false;
+    Product p{};
+    p.r_scales = (const unsigned char*)w_scales;
+    p.y = y;
+    p.pitch = pitch;
+    p.type = type;
+    p.wide = (uintptr_t)y % 16 == 0 && pitch * sizeof(T) % 16 == 0;
+    p.across = 1;
+    p.depth_blocks = (uint32_t)mx_blocks(k);
+    p.rows = (uint32_t)n;
+    p.cols = (uint32_t)m;
+    const Tokens in{x, x_pitch, (uint32_t)k, (uintptr_t)x % 16 == 0 && x_pitch * sizeof(T) % 16 == 0};
+    CUtensorMap map;
+    if (!operand_map(&map, w_codes, n, p.depth_blocks, kRows)) rc = ZCCL_E_CUDA;
+    else rc = launched(launch_cluster(parts, mx4_token_kernel<T>, dim3((unsigned)row_tiles * parts), dim3(kProductThreads), bytes, st, map, p, in));
+    return true;
+}
+
 // `weights_ready`: B was complete before the kernel in front on the stream started.
 int multiply(const void* a_codes, const void* a_scales, size_t m, const void* b_codes, const void* b_scales, size_t n, size_t k, void* y, int type, size_t pitch, bool weights_ready, void* stream)
 {
@@ -688,8 +878,15 @@ int zccl_mx4_matmul(const void* a_codes, const void* a_scales, size_t m, const v
 int zccl_mx4_linear(const void* x, int type, size_t m, size_t k, size_t x_pitch, const void* w_codes, const void* w_scales, size_t n, void* x_codes, void* x_scales, void* y, size_t pitch, void* stream)
 {
     if (m == 0 || n == 0 || k == 0) return multiply(x_codes, x_scales, m, w_codes, w_scales, n, k, y, type, pitch, false, stream);
-    if (!aligned16(w_codes) || !aligned16(w_scales) || pitch < n || !y || (uintptr_t)y % (type == ZCCL_F32 ? 4 : 2)) return ZCCL_E_ARG;
-    const int rc = zccl_mx4_quantize(x, type, m, k, x_pitch, 0, x_codes, x_scales, stream);
+    if (type < ZCCL_F32 || type > ZCCL_F16 || !aligned16(w_codes) || !aligned16(w_scales) || !aligned16(x_codes) || !aligned16(x_scales) || pitch < n || x_pitch < k) return ZCCL_E_ARG;
+    const size_t element = type == ZCCL_F32 ? 4 : 2;
+    if (!x || !y || (uintptr_t)x % element || (uintptr_t)y % element) return ZCCL_E_ARG;
+    cudaStream_t st = (cudaStream_t)stream;
+    int rc = ZCCL_OK;
+    if (type == ZCCL_F32 ? tokens((const float*)x, type, m, k, x_pitch, w_codes, w_scales, n, y, pitch, st, rc)
+        : type == ZCCL_BF16 ? tokens((const __nv_bfloat16*)x, type, m, k, x_pitch, w_codes, w_scales, n, y, pitch, st, rc)
+                            : tokens((const __half*)x, type, m, k, x_pitch, w_codes, w_scales, n, y, pitch, st, rc)) return rc;
+    rc = zccl_mx4_quantize(x, type, m, k, x_pitch, 0, x_codes, x_scales, stream);
     return rc == ZCCL_OK ? multiply(x_codes, x_scales, m, w_codes, w_scales, n, k, y, type, pitch, true, stream) : rc;
 }
 

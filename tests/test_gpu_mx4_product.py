@@ -196,6 +196,42 @@ def test_gradient_against_differences(mx):
                 assert f(up) - f(down) == 4.0 * float(grad[r, c])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("m", [1, 2, 3, 5, 8, 9, 13, 16, 17, 70, 129])
+def test_a_layer_with_held_weights_is_quantising_and_multiplying(mx, m, dtype):
+    """Few rows are quantised inside the product: the same bits, at every way in which the depth can end and for rows that begin anywhere."""
+    for k, n in ((1, 20), (31, 200), (64, 129), (127, 300), (129, 1000), (257, 300), (1000, 500), (2049, 700), (4161, 3000), (8192, 4096), (20000, 300)):
+        gen = torch.Generator().manual_seed(m * 31 + k)
+        w = mx.quantize(torch.randn(n, k, generator=gen).cuda())
+        for shift, pitch in ((0, k + (-k) % 8), (1, k + 3)):
+            flat = (torch.randn(m * pitch + 16, generator=gen) * torch.exp2(torch.randint(-5, 6, (m * pitch + 16,), generator=gen).float())).to(dtype).cuda()
+            x = flat[shift:shift + m * pitch].view(m, pitch)[:, :k]
+            assert torch.equal(mx.linear(x, w), mx.matmul(mx.quantize(x), w, dtype)), (k, n, shift)
+    assert mx.status() == 0
+
+
+def test_a_token_that_is_not_a_number_stays_alone(mx):
+    x = torch.randn(3, 600, device="cuda")
+    x[1, 5] = float("inf")
+    y = mx.linear(x, mx.quantize(torch.randn(500, 600, device="cuda")))
+    assert bool(torch.isnan(y[1]).all()) and bool(torch.isfinite(y[[0, 2]]).all())
+
+
+def test_layers_of_a_few_tokens_on_several_streams(mx):
+    x = [torch.randn(m, 4096, device="cuda", dtype=torch.bfloat16) for m in (1, 2, 4, 1, 3, 64)]
+    w = [mx.quantize(torch.randn(n, 4096, device="cuda")) for n in (4096, 3000, 500, 9000, 4096, 4096)]
+    want = [mx.linear(a, b) for a, b in zip(x, w)]
+    streams = [torch.cuda.Stream() for _ in x]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        got = []
+        for a, b, s in zip(x, w, streams):
+            with torch.cuda.stream(s):
+                got.append(mx.linear(a, b))
+    torch.cuda.synchronize()
+    assert mx.status() == 0 and all(torch.equal(p, q) for p, q in zip(want, got))
+
+
 def test_leading_dimensions_and_refusals(mx):
     x, w = torch.randn(2, 3, 64, device="cuda"), torch.randn(40, 64, device="cuda")
     y = mx.linear(x, w)
