@@ -361,13 +361,14 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
 
 // The layer of a few rows in one launch: mx4_split_kernel<16> across, whose CTAs quantise their piece of x themselves, into the places in shared memory
 // where a load would have put it, while the first weights are on their way.  A quantisation of its own takes 1.4 us and leaves the memory idle for
-// longer (1 x 8192 x 16384 with weights from memory: 17.2 us as two launches).  Every CTA quantises all of its piece, so there may not be much of it (kMostUnits).
+// longer: 1 x 8192 x 16384 with weights from memory 15.6 us, as two launches 17.2 us; 1 x 4096 x 4096 5.0 and 6.2 us.  Every CTA quantises all of its
+// piece, so there may not be much of it (kMostUnits; 8 x 2048 x 30000, 128 runs to a CTA, took 12.5 us instead of 10.1 us).
 struct TokenShape {
     using S = SplitShape<16>;
     static constexpr int kStages = S::kStages, kRowScaleAt = kRows * kRowBytes, kStage = kRowScaleAt + 2 * kMxTileBytes;
     // a depth tile of x: 16 rows of codes, and two tiles of scales of which 16 rows count; the rest of a tile is the next one's, or nothing
     static constexpr int kCodes = 16 * kRowBytes, kScales = 256;
-    static constexpr uint32_t kMostUnits = 128;                                  // runs of 128 elements of a row
+    static constexpr uint32_t kMostUnits = 48;                                   // runs of 128 elements of a row: what 12 half-warps load at once
     static constexpr size_t kMostBytes = 112 * 1024;                             // two CTAs to an SM
     static size_t bytes(size_t depth_tiles) { return (size_t)kStage * kStages + depth_tiles * (kCodes + 2 * kScales) + kMxTileBytes + 1024; }
     static_assert(16 * kRows * 4 <= kStage * kStages, "sums take the stages' place");
