@@ -283,6 +283,7 @@ bool matrix(PyObject* o, const at::Tensor** t, int* type, size_t* pitch)
     if (!cuda_tensor(o, t)) return false;
     *type = type_of(**t);
     if (*type < 0) return refuse("expected float32, bfloat16 or float16");
+    if ((*t)->layout() != c10::kStrided || (*t)->is_neg()) return refuse("expected a dense tensor");
     if ((*t)->dim() != 2 || ((*t)->size(1) > 1 && (*t)->stride(1) != 1) || ((*t)->size(0) > 1 && (*t)->stride(0) < (*t)->size(1)))
         return refuse("expected a matrix with contiguous rows");
     *pitch = (*t)->size(0) > 1 ? (size_t)(*t)->stride(0) : (size_t)(*t)->size(1);
@@ -316,18 +317,6 @@ bool stream_on(PyObject* o, const at::Tensor& t, void** st)
     if (index != t.device().index()) return refuse("the stream is of another device than the tensors");
     return stream_of(o, st);
 }
-template <class F>
-PyObject* status_on(const at::Tensor& t, F&& f)
-{
-    try {
-        const c10::cuda::CUDAGuard guard(t.device());
-        return status(f);
-    } catch (const std::exception& e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
-        return nullptr;
-    }
-}
-
 // A list or tuple of tensors, kept alive by its caller.
 struct Tensors {
     PyObject* seq = nullptr;
@@ -355,18 +344,6 @@ struct Place {
         return true;
     }
 };
-// Runs what allocates or launches; C++ exceptions end here.
-template <class F>
-PyObject* guarded(F&& f)
-{
-    try {
-        return f();
-    } catch (const std::exception& e) {
-        if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
-        return nullptr;
-    }
-}
-
 at::Tensor new_bytes(size_t n, const at::Tensor& like) { return at::detail::empty_cuda({(int64_t)n}, at::kByte, like.device(), c10::nullopt); }
 at::Tensor new_matrix(size_t rows, size_t cols, c10::ScalarType dt, const at::Tensor& like) { return at::detail::empty_cuda({(int64_t)rows, (int64_t)cols}, dt, like.device(), c10::nullopt); }
 struct Form {
@@ -432,14 +409,12 @@ PyObject* mx4_quantize(PyObject*, Args a, Py_ssize_t na)
     Form f;
     const bool given = a[2] != Py_None;
     if (given && !take_form(a[2], a[3], rows, cols, *x.t, &f)) return nullptr;
-    return guarded([&]() -> PyObject* {
-        Place place;
-        if (!place.take(a[4], *x.t)) return nullptr;
-        if (!given) f = new_form(rows, cols, *x.t);
-        const int rc = x.quantize(transpose, f, place.st);
-        if (rc != ZCCL_OK) return PyLong_FromLong(rc);
-        return Py_BuildValue("NN", THPVariable_Wrap(f.codes), THPVariable_Wrap(f.scales));
-    });
+    Place place;
+    if (!place.take(a[4], *x.t)) return nullptr;
+    if (!given) f = new_form(rows, cols, *x.t);
+    const int rc = x.quantize(transpose, f, place.st);
+    if (rc != ZCCL_OK) return PyLong_FromLong(rc);
+    return Py_BuildValue("NN", THPVariable_Wrap(f.codes), THPVariable_Wrap(f.scales));
 }
 
 // (matrices, transposes, stream) -> list of (codes, scales) or a status
@@ -458,20 +433,18 @@ PyObject* mx4_quantize_all(PyObject*, Args a, Py_ssize_t na)
         if (x[i].type != x[0].type || x[i].t->device() != x[0].t->device()) return refuse("all matrices of a call are of one type and on one device"), nullptr;
     }
     if (count == 0) return PyList_New(0);
-    return guarded([&]() -> PyObject* {
-        Place place;
-        if (!place.take(a[2], *x[0].t)) return nullptr;
-        for (size_t i = 0; i < count; ++i) {
-            const bool transpose = PyObject_IsTrue(PySequence_Fast_GET_ITEM(ts.seq, (Py_ssize_t)i)) == 1;
-            f[i] = transpose ? new_form(x[i].cols, x[i].rows, *x[0].t) : new_form(x[i].rows, x[i].cols, *x[0].t);
-            jobs[i] = x[i].job(transpose, f[i]);
-        }
-        const int rc = zccl_mx4_quantize_all(jobs.data(), (int)count, x[0].type, place.st);
-        if (rc != ZCCL_OK) return PyLong_FromLong(rc);
-        PyObject* const out = PyList_New((Py_ssize_t)count);
-        for (size_t i = 0; out && i < count; ++i) PyList_SET_ITEM(out, (Py_ssize_t)i, Py_BuildValue("NN", THPVariable_Wrap(f[i].codes), THPVariable_Wrap(f[i].scales)));
-        return out;
-    });
+    Place place;
+    if (!place.take(a[2], *x[0].t)) return nullptr;
+    for (size_t i = 0; i < count; ++i) {
+        const bool transpose = PyObject_IsTrue(PySequence_Fast_GET_ITEM(ts.seq, (Py_ssize_t)i)) == 1;
+        f[i] = transpose ? new_form(x[i].cols, x[i].rows, *x[0].t) : new_form(x[i].rows, x[i].cols, *x[0].t);
+        jobs[i] = x[i].job(transpose, f[i]);
+    }
+    const int rc = zccl_mx4_quantize_all(jobs.data(), (int)count, x[0].type, place.st);
+    if (rc != ZCCL_OK) return PyLong_FromLong(rc);
+    PyObject* const out = PyList_New((Py_ssize_t)count);
+    for (size_t i = 0; out && i < count; ++i) PyList_SET_ITEM(out, (Py_ssize_t)i, Py_BuildValue("NN", THPVariable_Wrap(f[i].codes), THPVariable_Wrap(f[i].scales)));
+    return out;
 }
 
 // (codes, scales, rows, cols, dtype, y or None, stream) -> y or a status
@@ -489,12 +462,10 @@ PyObject* mx4_dequantize(PyObject*, Args a, Py_ssize_t na)
         if (!y.take(a[5])) return nullptr;
         if (y.rows != rows || y.cols != cols || y.t->device() != codes->device()) return refuse("the output is of another size or device than the form"), nullptr;
     } else if (!element_type(a[4], &dt)) return nullptr;
-    return guarded([&]() -> PyObject* {
-        Place place;
-        if (!place.take(a[6], *codes)) return nullptr;
-        const at::Tensor out = given ? *y.t : new_matrix(rows, cols, dt, *codes);
-        return wrapped(zccl_mx4_dequantize(f.codes.data_ptr(), f.scales.data_ptr(), rows, cols, out.data_ptr(), type_of(out), given ? y.pitch : cols, place.st), out);
-    });
+    Place place;
+    if (!place.take(a[6], *codes)) return nullptr;
+    const at::Tensor out = given ? *y.t : new_matrix(rows, cols, dt, *codes);
+    return wrapped(zccl_mx4_dequantize(f.codes.data_ptr(), f.scales.data_ptr(), rows, cols, out.data_ptr(), type_of(out), given ? y.pitch : cols, place.st), out);
 }
 
 // (a_codes, a_scales, m, b_codes, b_scales, n, k, dtype, y or None, stream) -> y or a status
@@ -512,12 +483,10 @@ PyObject* mx4_matmul(PyObject*, Args a, Py_ssize_t na)
         if (!y.take(a[8])) return nullptr;
         if (y.rows != m || y.cols != n || y.t->device() != codes->device()) return refuse("the output is of another size or device than the operands"), nullptr;
     } else if (!element_type(a[7], &dt)) return nullptr;
-    return guarded([&]() -> PyObject* {
-        Place place;
-        if (!place.take(a[9], *codes)) return nullptr;
-        const at::Tensor out = given ? *y.t : new_matrix(m, n, dt, *codes);
-        return wrapped(zccl_mx4_matmul(l.codes.data_ptr(), l.scales.data_ptr(), m, r.codes.data_ptr(), r.scales.data_ptr(), n, k, out.data_ptr(), type_of(out), given ? y.pitch : n, place.st), out);
-    });
+    Place place;
+    if (!place.take(a[9], *codes)) return nullptr;
+    const at::Tensor out = given ? *y.t : new_matrix(m, n, dt, *codes);
+    return wrapped(zccl_mx4_matmul(l.codes.data_ptr(), l.scales.data_ptr(), m, r.codes.data_ptr(), r.scales.data_ptr(), n, k, out.data_ptr(), type_of(out), given ? y.pitch : n, place.st), out);
 }
 
 // (x, w) or (x, codes, scales, n) -> x W^T in x's type, or a status
@@ -536,21 +505,19 @@ PyObject* mx4_linear(PyObject*, Args a, Py_ssize_t na)
         n = PyLong_AsSize_t(a[3]);
         if (PyErr_Occurred() || !take_form(a[1], a[2], n, x.cols, *x.t, &held)) return nullptr;
     }
-    return guarded([&]() -> PyObject* {
-        Place place;
-        if (!place.take(Py_None, *x.t)) return nullptr;
-        const Form f = new_form(x.rows, x.cols, *x.t);
-        const at::Tensor y = new_matrix(x.rows, n, x.t->scalar_type(), *x.t);
-        int rc;
-        if (na == 2) {
-            held = new_form(n, x.cols, *x.t);
-            const zccl_mx4_job both[2] = {w.job(false, held), x.job(false, f)};
-            rc = zccl_mx4_quantize_all(both, 2, x.type, place.st);
-            if (rc == ZCCL_OK) rc = multiply(f, x.rows, held, n, x.cols, y, place.st);
-        } else
-            rc = zccl_mx4_linear(x.t->data_ptr(), x.type, x.rows, x.cols, x.pitch, held.codes.data_ptr(), held.scales.data_ptr(), n, f.codes.data_ptr(), f.scales.data_ptr(), y.data_ptr(), n, place.st);
-        return wrapped(rc, y);
-    });
+    Place place;
+    if (!place.take(Py_None, *x.t)) return nullptr;
+    const Form f = new_form(x.rows, x.cols, *x.t);
+    const at::Tensor y = new_matrix(x.rows, n, x.t->scalar_type(), *x.t);
+    int rc;
+    if (na == 2) {
+        held = new_form(n, x.cols, *x.t);
+        const zccl_mx4_job both[2] = {w.job(false, held), x.job(false, f)};
+        rc = zccl_mx4_quantize_all(both, 2, x.type, place.st);
+        if (rc == ZCCL_OK) rc = multiply(f, x.rows, held, n, x.cols, y, place.st);
+    } else
+        rc = zccl_mx4_linear(x.t->data_ptr(), x.type, x.rows, x.cols, x.pitch, held.codes.data_ptr(), held.scales.data_ptr(), n, f.codes.data_ptr(), f.scales.data_ptr(), y.data_ptr(), n, place.st);
+    return wrapped(rc, y);
 }
 
 // (dy, x, w, dx wanted, dw wanted) -> (dx or None, dw or None), or a status
@@ -563,46 +530,44 @@ PyObject* mx4_linear_backward(PyObject*, Args a, Py_ssize_t na)
     if (dy.rows != m || dy.cols != n || w.cols != k) return refuse("sizes of the gradient, the input and the weights do not belong together"), nullptr;
     if (dy.t->device() != x.t->device() || w.t->device() != x.t->device()) return refuse("all tensors of a call are on one device"), nullptr;
     const bool want_x = PyObject_IsTrue(a[3]) == 1, want_w = PyObject_IsTrue(a[4]) == 1;
-    return guarded([&]() -> PyObject* {
-        Place place;
-        if (!place.take(Py_None, *x.t)) return nullptr;
-        at::Tensor dx, dw;
-        Form xl, xr, wl, wr;
-        zccl_mx4_job jobs[4];
-        int count = 0;
-        if (want_x) {
-            xl = new_form(m, n, *x.t);
-            xr = new_form(k, n, *x.t);
-            dx = new_matrix(m, k, x.t->scalar_type(), *x.t);
-            jobs[count++] = dy.job(false, xl);
-            jobs[count++] = w.job(true, xr);
-        }
-        if (want_w) {
-            wl = new_form(n, m, *x.t);
-            wr = new_form(k, m, *x.t);
-            dw = new_matrix(n, k, w.t->scalar_type(), *x.t);
-            jobs[count++] = dy.job(true, wl);
-            jobs[count++] = x.job(true, wr);
-        }
-        int rc = ZCCL_OK;
-        if (dy.type == x.type && w.type == x.type) rc = zccl_mx4_quantize_all(jobs, count, x.type, place.st);
-        else {
-            if (want_x) rc = dy.quantize(false, xl, place.st);
-            if (want_x && rc == ZCCL_OK) rc = w.quantize(true, xr, place.st);
-            if (want_w && rc == ZCCL_OK) rc = dy.quantize(true, wl, place.st);
-            if (want_w && rc == ZCCL_OK) rc = x.quantize(true, wr, place.st);
-        }
-        if (want_x && rc == ZCCL_OK) rc = multiply(xl, m, xr, k, n, dx, place.st);
-        if (want_w && rc == ZCCL_OK) rc = multiply(wl, n, wr, k, m, dw, place.st);
-        if (rc != ZCCL_OK) return PyLong_FromLong(rc);
-        Py_INCREF(Py_None);
-        Py_INCREF(Py_None);
-        PyObject* const ox = want_x ? THPVariable_Wrap(dx) : Py_None;
-        PyObject* const ow = want_w ? THPVariable_Wrap(dw) : Py_None;
-        if (want_x) Py_DECREF(Py_None);
-        if (want_w) Py_DECREF(Py_None);
-        return Py_BuildValue("NN", ox, ow);
-    });
+    Place place;
+    if (!place.take(Py_None, *x.t)) return nullptr;
+    at::Tensor dx, dw;
+    Form xl, xr, wl, wr;
+    zccl_mx4_job jobs[4];
+    int count = 0;
+    if (want_x) {
+        xl = new_form(m, n, *x.t);
+        xr = new_form(k, n, *x.t);
+        dx = new_matrix(m, k, x.t->scalar_type(), *x.t);
+        jobs[count++] = dy.job(false, xl);
+        jobs[count++] = w.job(true, xr);
+    }
+    if (want_w) {
+        wl = new_form(n, m, *x.t);
+        wr = new_form(k, m, *x.t);
+        dw = new_matrix(n, k, w.t->scalar_type(), *x.t);
+        jobs[count++] = dy.job(true, wl);
+        jobs[count++] = x.job(true, wr);
+    }
+    int rc = ZCCL_OK;
+    if (dy.type == x.type && w.type == x.type) rc = zccl_mx4_quantize_all(jobs, count, x.type, place.st);
+    else {
+        if (want_x) rc = dy.quantize(false, xl, place.st);
+        if (want_x && rc == ZCCL_OK) rc = w.quantize(true, xr, place.st);
+        if (want_w && rc == ZCCL_OK) rc = dy.quantize(true, wl, place.st);
+        if (want_w && rc == ZCCL_OK) rc = x.quantize(true, wr, place.st);
+    }
+    if (want_x && rc == ZCCL_OK) rc = multiply(xl, m, xr, k, n, dx, place.st);
+    if (want_w && rc == ZCCL_OK) rc = multiply(wl, n, wr, k, m, dw, place.st);
+    if (rc != ZCCL_OK) return PyLong_FromLong(rc);
+    Py_INCREF(Py_None);
+    Py_INCREF(Py_None);
+    PyObject* const ox = want_x ? THPVariable_Wrap(dx) : Py_None;
+    PyObject* const ow = want_w ? THPVariable_Wrap(dw) : Py_None;
+    if (want_x) Py_DECREF(Py_None);
+    if (want_w) Py_DECREF(Py_None);
+    return Py_BuildValue("NN", ox, ow);
 }
 
 // Entry i of a list that belongs to `like`: contiguous, of type `dt`, `n` elements, on the same device.
@@ -741,17 +706,18 @@ PyObject* adamw(PyObject*, Args a, Py_ssize_t na)
         k.norm = (const float*)t->data_ptr();
         k.max_norm = PyFloat_AsDouble(a[15]);
     }
-    void* st;
-    if (PyErr_Occurred() || !stream_on(a[16], *first, &st)) return nullptr;
-    PyObject* rc = status_on(*first, [&] { return zccl_adamw(list.data(), count, &k, st); });
+    if (PyErr_Occurred()) return nullptr;
+    Place place;
+    if (!place.take(a[16], *first)) return nullptr;
+    const int rc = zccl_adamw(list.data(), count, &k, place.st);
     // parameters and copies may have been saved for a backward pass
-    for (size_t i = 0; i < count; ++i)
+    for (size_t i = 0; rc == ZCCL_OK && i < count; ++i)
         for (const Tensors* l : {&p, copied ? &copies : nullptr})
             if (l) {
                 const at::Tensor& x = THPVariable_Unpack(PySequence_Fast_GET_ITEM(l->seq, (Py_ssize_t)i));
                 if (!x.is_inference()) x.unsafeGetTensorImpl()->bump_version();
             }
-    return rc;
+    return PyLong_FromLong(rc);
 }
 
 // (grads, norm or None, stream) -> norm or a status
@@ -776,22 +742,33 @@ PyObject* grad_norm(PyObject*, Args a, Py_ssize_t na)
         at[i] = t->data_ptr();
         n[i] = (size_t)t->numel();
     }
-    return guarded([&]() -> PyObject* {
-        Place place;
-        if (!place.take(a[2], like)) return nullptr;
-        const at::Tensor out = given ? *norm : at::Tensor(at::detail::empty_cuda({1}, c10::kFloat, like.device(), c10::nullopt));
-        const at::Tensor work = new_bytes(zccl_grad_norm_work(count), like);
-        return wrapped(zccl_grad_norm(at.data(), n.data(), count, type, (float*)out.data_ptr(), work.data_ptr(), place.st), out);
-    });
+    Place place;
+    if (!place.take(a[2], like)) return nullptr;
+    const at::Tensor out = given ? *norm : at::Tensor(at::detail::empty_cuda({1}, c10::kFloat, like.device(), c10::nullopt));
+    const at::Tensor work = new_bytes(zccl_grad_norm_work(count), like);
+    return wrapped(zccl_grad_norm(at.data(), n.data(), count, type, (float*)out.data_ptr(), work.data_ptr(), place.st), out);
 }
 
+// What torch throws (a tensor without memory or strides of its own, no memory left) ends here as a Python exception.
+template <PyObject* (*F)(PyObject*, Args, Py_ssize_t)>
+PyObject* guarded(PyObject* self, Args a, Py_ssize_t na)
+{
+    try {
+        return F(self, a, na);
+    } catch (const std::exception& e) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+#define GUARDED(name) {#name, (PyCFunction)(void (*)(void))guarded<name>, METH_FASTCALL, nullptr}
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     {"current_stream", current_stream, METH_NOARGS, nullptr},
     FAST(compress), FAST(decompress), FAST(hop), FAST(compress_f64), FAST(decompress_f64), FAST(compress_tiled), FAST(decompress_tiled), FAST(sim_allreduce),
     {"sim_allgather", (PyCFunction)(void (*)(void))sim<zccl_sim_allgather>, METH_FASTCALL, nullptr},
     {"sim_reduce_scatter", (PyCFunction)(void (*)(void))sim<zccl_sim_reduce_scatter>, METH_FASTCALL, nullptr},
-    FAST(mx4_sizes), FAST(mx4_quantize), FAST(mx4_quantize_all), FAST(mx4_dequantize), FAST(mx4_matmul), FAST(mx4_linear), FAST(mx4_linear_backward), FAST(adamw), FAST(grad_norm),
+    GUARDED(mx4_sizes), GUARDED(mx4_quantize), GUARDED(mx4_quantize_all), GUARDED(mx4_dequantize), GUARDED(mx4_matmul), GUARDED(mx4_linear), GUARDED(mx4_linear_backward), GUARDED(adamw), GUARDED(grad_norm),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_zccl", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(kOptThreads) norm_parts_kernel(const __grid_co
     }
 }
 
-__global__ void __launch_bounds__(kOptThreads) norm_join_kernel(const double* __restrict__ parts, uint32_t count, float* __restrict__ norm)
+__global__ void __launch_bounds__(kOptThreads) norm_join_kernel(const double* parts, uint32_t count, float* norm)
 {
     pdl_enter();
     double sum = 0.0;
@@ -324,11 +324,11 @@ __device__ __forceinline__ uint2 pack8(float (&v)[8], const uint32_t (&noise)[8]
     return make_uint2(prmt(prmt(z[0], z[1], 0x0073), prmt(z[2], z[3], 0x0073), 0x5410), prmt(prmt(z[4], z[5], 0x0073), prmt(z[6], z[7], 0x0073), 0x5410));
 }
 
-// Both to within 2^-22; subnormal numbers count as zero.
+// Both to within 2^-22.  A root of a subnormal number is one (gradients of 1e-19 square to these); no root is subnormal itself, so no quotient is by one.
 __device__ __forceinline__ float root_of(float v)
 {
     float r;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
 __device__ __forceinline__ float reciprocal_of(float v)

@@ -14,7 +14,8 @@ from . import zccl as z
 
 
 class Mx4(NamedTuple):
-    """A matrix [rows, cols] in microscaled form: `codes` (uint8, code_bytes) and `scales` (uint8, scale_bytes), any shape."""
+    """A matrix [rows, cols] in microscaled form: `codes` (uint8, code_bytes) and `scales` (uint8, scale_bytes), any shape, laid out as
+    ``include/zccl.h`` says (zeros behind the last row and block of the scales)."""
 
     codes: torch.Tensor
     scales: torch.Tensor

@@ -34,13 +34,14 @@ def exchange(ring, grads, eb_mode: int, eb: float) -> list[torch.Tensor]:
     """The gradients' average over the ranks of `ring` (a `ring.Ring`), compressed on the way: one Allreduce of all of them, as float32, in
     which every rank ends with the same values (ZCCL_CONSISTENT_OWNER).  Returns tensors of the gradients' shapes, views of one array in which each
     begins at a multiple of 32 elements; the gaps hold zeros, which count into the range that a relative bound refers to."""
-    at, spans = 0, []
+    at, spans, grads = 0, [], list(grads)
+    if not grads:
+        return []
     for g in grads:
         spans.append((at, g.numel()))
         at += -(-g.numel() // BLOCK) * BLOCK
     flat = torch.zeros(at, dtype=torch.float32, device=ring.codec.device)
-    if spans:
-        torch._foreach_copy_([flat[o:o + n].view(g.shape) for (o, n), g in zip(spans, grads)], list(grads))
+    torch._foreach_copy_([flat[o:o + n].view(g.shape) for (o, n), g in zip(spans, grads)], grads)
     reduced = torch.empty_like(flat)
     ring.allreduce(flat, reduced, eb_mode, eb, flags=z.OP_AVG | z.CONSISTENT_OWNER)
     return [reduced[o:o + n].view(g.shape) for (o, n), g in zip(spans, grads)]

@@ -113,6 +113,25 @@ def test_a_large_matrix(mx, transpose):
     assert torch.equal(got, want.to(torch.bfloat16))
 
 
+def test_offsets_beyond_32_bits(mx):
+    """A matrix of more than 2^32 elements, along its rows and along its columns, at its last rows and columns."""
+    rows, cols = 70_001, 65_536
+    x = torch.zeros(rows, cols, device="cuda", dtype=torch.bfloat16)
+    end = data(33, cols, torch.bfloat16, 5)
+    x[-33:] = end.cuda()
+    q = mx.quantize(x)
+    y = mx.dequantize(q, torch.bfloat16)
+    want, s = ref.quantize(wide(end))
+    assert torch.equal(y[-33:].cpu(), torch.from_numpy(ref.values(want, s, cols)).bfloat16()) and not y[: 1 << 12].any()
+    del q, y
+    q = mx.quantize(x, transpose=True)                  # [65536, 70001]
+    y = mx.dequantize(q, torch.bfloat16)
+    part = torch.zeros(64, 96, dtype=torch.bfloat16)    # the last 64 columns' last 81 elements, from a block's begin on
+    part[:, :81] = x[rows - 81:, cols - 64:].t().cpu()
+    want, s = ref.quantize(wide(part))
+    assert (rows - 81) % 32 == 0 and torch.equal(y[-64:, rows - 81:].cpu(), torch.from_numpy(ref.values(want, s, 96)[:, :81]).bfloat16())
+
+
 def test_streams_graphs_and_buffers_that_are_given(mx):
     x = data(70, 200, torch.float32, 1).cuda()
     want = mx.quantize(x)
@@ -173,6 +192,10 @@ def test_refusals(mx):
         mx.dequantize(q, torch.float64)
     with pytest.raises(ValueError):
         mx.dequantize(q, out=torch.empty(4, 32, device="cuda"))
+    with pytest.raises(ValueError):
+        mx.quantize(x.to_sparse())
+    with pytest.raises(ValueError):
+        mx.quantize(torch._neg_view(x))
     with pytest.raises(RuntimeError):                              # codes that begin on no 16-byte boundary
         buffer = torch.zeros(q.codes.numel() + 1, dtype=torch.uint8, device="cuda")
         mx.dequantize(mx.Mx4(buffer[1:], q.scales, 4, 64))

@@ -68,7 +68,7 @@ def test_few_rows(mx, m, n):
     product(mx, n, m, 700, torch.float16, m)
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 16384, 8192), (3, 5000, 20000), (13, 10007, 4161), (128, 257, 9000), (130, 140, 16384), (500, 600, 300), (777, 1531, 1000), (2049, 3001, 520), (4097, 2500, 321), (12800, 400, 512), (6000, 6001, 100)])
+@pytest.mark.parametrize("m,n,k", [(1, 16384, 8192), (3, 5000, 20000), (2, 200, 300_000), (13, 10007, 4161), (128, 257, 9000), (130, 140, 16384), (500, 600, 300), (777, 1531, 1000), (2049, 3001, 520), (4097, 2500, 321), (12800, 400, 512), (6000, 6001, 100)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_shapes(mx, m, n, k, dtype):
     product(mx, m, n, k, dtype, 5)
@@ -76,6 +76,13 @@ def test_shapes(mx, m, n, k, dtype):
 
 def test_large(mx):
     product(mx, 4096, 8192, 8192, torch.bfloat16, 9)
+
+
+def test_an_output_beyond_32_bits(mx):
+    a, b = operand(70_001, 32, 1), operand(65_536, 32, 2)
+    y = mx.matmul(mx.Mx4(a[0], a[1], 70_001, 32), mx.Mx4(b[0], b[1], 65_536, 32), torch.bfloat16)
+    for rows in (slice(0, 130), slice(65_400, 65_700), slice(69_900, 70_001)):
+        close(y[rows], a[2][rows], b[2])
 
 
 def test_scales_of_every_size(mx):

@@ -174,6 +174,50 @@ def test_a_norm_that_is_not_finite_leaves_everything(optim, bits, norm):
     assert all(torch.equal(a, b) for a, b in zip(before, flat_bytes(s))) and all(bool((c == 5.0).all()) for c in copies)
 
 
+@pytest.mark.parametrize("scale", [1e15, 1e-13])
+def test_large_and_small_gradients(optim, scale):
+    """Blocks whose powers of two are far from 1 (at 1e15 the scale's reciprocal is applied in two steps)."""
+    for bits in (32, 8):
+        s = tensors([5000, 77], torch.float32, torch.float32, bits)
+        for k in ("g", "m", "v"):
+            for x in s[k]:
+                if bits == 32 or k == "g":
+                    x.mul_(scale * scale if k == "v" else scale)
+        if bits == 8:
+            for k in ("ms", "vs"):
+                for x in s[k]:
+                    x.add_(int(np.round(np.log2(scale))))
+        before = snapshot(s, bits)
+        run(optim, s, seed=21)
+        check(s, before, HYPER, bits, seed=21)
+
+
+def test_offsets_beyond_32_bits(optim):
+    """A tensor of 2^32 elements and some behind another one, states in 8 bits: its end against the reference, random bits by their place included."""
+    n, first = (1 << 32) + 77, 45
+    make = lambda k, dtype: torch.zeros(k, dtype=dtype, device="cuda")  # noqa: E731
+    s = {key: [make(first, dtype), make(n, dtype)] for key, dtype in (("p", torch.bfloat16), ("g", torch.bfloat16), ("m", torch.float8_e4m3fn), ("v", torch.float8_e4m3fn))}
+    s |= {key: [make(2, torch.uint8), make(-(-n // 32), torch.uint8)] for key in ("ms", "vs")}
+    tail = 4096 + 77
+    g = (torch.randn(tail, generator=torch.Generator().manual_seed(3)) * 1e-2).bfloat16().cuda()
+    s["g"][1][n - tail:] = g
+    s["p"][1][n - tail:] = 1.0
+    norm = optim.grad_norm(s["g"])
+    want_norm = np.sqrt((wide(g) ** 2).sum())
+    assert abs(float(norm) - want_norm) <= 6 * U * want_norm
+    run(optim, s, seed=8)
+    want_p, want_m, want_v = ref.step_of(np.ones(tail), wide(g), np.zeros(tail), np.zeros(tail), **HYPER)
+    dp, _, _ = bounds(np.ones(tail), wide(g), np.zeros(tail), np.zeros(tail), HYPER)
+    assert (np.abs(wide(s["p"][1][n - tail:]) - want_p) <= dp + (np.abs(want_p) + dp) * HALF[torch.bfloat16]).all()
+    random = ref.random_bits(8, HYPER["step"], np.arange(n - tail, n, dtype=np.uint64) + np.uint64(64))
+    for key, x, part, root in (("m", want_m, random >> np.uint64(16), False), ("v", np.sqrt(want_v), random & np.uint64(0xFFFF), True)):
+        want, scale, _ = ref.encode8(x, part.astype(np.float64), root)
+        got = wide(s[key][1][n - tail:]) * np.repeat(np.ldexp(1.0, s[key + "s"][1][(n - tail) // 32:].cpu().numpy().astype(int) - 127), 32)[:tail]
+        off = np.count_nonzero(got != want * np.repeat(np.ldexp(1.0, scale - 127), 32)[:tail])
+        assert off <= 2      # see check(): a chance of 2^-15 per element
+    assert not s["p"][1][:1 << 20].any() and not s["m"][1][1 << 31:(1 << 31) + (1 << 20)].view(torch.uint8).any()
+
+
 def test_a_gradient_that_is_not_finite_stays_in_its_block(optim):
     for bits in (32, 8):
         s = tensors([200], torch.float32, torch.float32, bits)
@@ -360,6 +404,11 @@ def test_refusals(optim):
         run(optim, fresh(), step=0)
     with pytest.raises(RuntimeError):
         run(optim, fresh(), betas=(0.9, 1.0))
+    for other in (t(64).to_sparse(), torch.zeros(64, device="meta")):
+        with pytest.raises((ValueError, RuntimeError)):
+            run(optim, fresh(g=[other, t(32)]))
+        with pytest.raises((ValueError, RuntimeError)):
+            optim.grad_norm([other])
     s = tensors([64, 32], torch.float32, torch.float32, 8)
     s["vs"][0] = s["vs"][0][:1]
     with pytest.raises(ValueError):
