@@ -362,15 +362,36 @@ struct Matrix {
         cols = (size_t)t->size(1);
         return true;
     }
-    zccl_mx4_job job(bool transpose, const Form& f) const { return {t->data_ptr(), rows, cols, pitch, transpose, f.codes.data_ptr(), f.scales.data_ptr()}; }
-    int quantize(bool transpose, const Form& f, void* st) const
+    zccl_mx4_job job(bool transpose, void* codes, void* scales) const { return {t->data_ptr(), rows, cols, pitch, transpose, codes, scales}; }
+    int quantize(bool transpose, void* codes, void* scales, void* st) const { return zccl_mx4_quantize(t->data_ptr(), type, rows, cols, pitch, transpose, codes, scales, st); }
+};
+// Forms that a call needs for itself, out of one allocation: each costs the host as much as a small kernel costs the GPU.
+struct Inner {
+    void *codes = nullptr, *scales = nullptr;
+};
+struct InnerForms {
+    size_t bytes = 0;
+    struct { size_t codes, scales; } at[4];
+    int count = 0;
+    void add(size_t rows, size_t cols)
     {
-        return zccl_mx4_quantize(t->data_ptr(), type, rows, cols, pitch, transpose, f.codes.data_ptr(), f.scales.data_ptr(), st);
+        const auto whole = [](size_t n) { return (n + 511) / 512 * 512; };
+        at[count].codes = bytes;
+        bytes += whole(zccl_mx4_code_bytes(rows, cols));
+        at[count++].scales = bytes;
+        bytes += whole(zccl_mx4_scale_bytes(rows, cols));
+    }
+    at::Tensor memory;
+    void take(const at::Tensor& like) { memory = new_bytes(bytes, like); }
+    Inner operator[](int i) const
+    {
+        char* const base = (char*)memory.data_ptr();
+        return {base + at[i].codes, base + at[i].scales};
     }
 };
-int multiply(const Form& a, size_t m, const Form& b, size_t n, size_t k, const at::Tensor& y, void* st)
+int multiply(const Inner& a, size_t m, const Inner& b, size_t n, size_t k, const at::Tensor& y, void* st)
 {
-    return zccl_mx4_matmul(a.codes.data_ptr(), a.scales.data_ptr(), m, b.codes.data_ptr(), b.scales.data_ptr(), n, k, y.data_ptr(), type_of(y), n, st);
+    return zccl_mx4_matmul(a.codes, a.scales, m, b.codes, b.scales, n, k, y.data_ptr(), type_of(y), n, st);
 }
 // A form that the caller has: bytes of the right number on the right device.
 bool take_form(PyObject* codes, PyObject* scales, size_t rows, size_t cols, const at::Tensor& like, Form* f)
@@ -398,7 +419,7 @@ PyObject* mx4_sizes(PyObject*, Args a, Py_ssize_t na)
     return Py_BuildValue("nn", (Py_ssize_t)zccl_mx4_code_bytes(rows, cols), (Py_ssize_t)zccl_mx4_scale_bytes(rows, cols));
 }
 
-// (x, transpose, codes or None, scales or None, stream) -> (codes, scales) or a status
+// (x, transpose, codes or None, scales or None, stream) -> (codes, scales, rows, cols) or a status
 PyObject* mx4_quantize(PyObject*, Args a, Py_ssize_t na)
 {
     if (!nargs_are(na, 5)) return nullptr;
@@ -412,9 +433,9 @@ PyObject* mx4_quantize(PyObject*, Args a, Py_ssize_t na)
     Place place;
     if (!place.take(a[4], *x.t)) return nullptr;
     if (!given) f = new_form(rows, cols, *x.t);
-    const int rc = x.quantize(transpose, f, place.st);
+    const int rc = x.quantize(transpose, f.codes.data_ptr(), f.scales.data_ptr(), place.st);
     if (rc != ZCCL_OK) return PyLong_FromLong(rc);
-    return Py_BuildValue("NN", THPVariable_Wrap(f.codes), THPVariable_Wrap(f.scales));
+    return Py_BuildValue("NNnn", THPVariable_Wrap(f.codes), THPVariable_Wrap(f.scales), (Py_ssize_t)rows, (Py_ssize_t)cols);
 }
 
 // (matrices, transposes, stream) -> list of (codes, scales) or a status
@@ -438,7 +459,7 @@ PyObject* mx4_quantize_all(PyObject*, Args a, Py_ssize_t na)
     for (size_t i = 0; i < count; ++i) {
         const bool transpose = PyObject_IsTrue(PySequence_Fast_GET_ITEM(ts.seq, (Py_ssize_t)i)) == 1;
         f[i] = transpose ? new_form(x[i].cols, x[i].rows, *x[0].t) : new_form(x[i].rows, x[i].cols, *x[0].t);
-        jobs[i] = x[i].job(transpose, f[i]);
+        jobs[i] = x[i].job(transpose, f[i].codes.data_ptr(), f[i].scales.data_ptr());
     }
     const int rc = zccl_mx4_quantize_all(jobs.data(), (int)count, x[0].type, place.st);
     if (rc != ZCCL_OK) return PyLong_FromLong(rc);
@@ -507,16 +528,20 @@ PyObject* mx4_linear(PyObject*, Args a, Py_ssize_t na)
     }
     Place place;
     if (!place.take(Py_None, *x.t)) return nullptr;
-    const Form f = new_form(x.rows, x.cols, *x.t);
+    InnerForms inner;
+    inner.add(x.rows, x.cols);
+    if (na == 2) inner.add(n, x.cols);
+    inner.take(*x.t);
+    const Inner f = inner[0];
     const at::Tensor y = new_matrix(x.rows, n, x.t->scalar_type(), *x.t);
     int rc;
     if (na == 2) {
-        held = new_form(n, x.cols, *x.t);
-        const zccl_mx4_job both[2] = {w.job(false, held), x.job(false, f)};
+        const Inner g = inner[1];
+        const zccl_mx4_job both[2] = {w.job(false, g.codes, g.scales), x.job(false, f.codes, f.scales)};
         rc = zccl_mx4_quantize_all(both, 2, x.type, place.st);
-        if (rc == ZCCL_OK) rc = multiply(f, x.rows, held, n, x.cols, y, place.st);
+        if (rc == ZCCL_OK) rc = multiply(f, x.rows, g, n, x.cols, y, place.st);
     } else
-        rc = zccl_mx4_linear(x.t->data_ptr(), x.type, x.rows, x.cols, x.pitch, held.codes.data_ptr(), held.scales.data_ptr(), n, f.codes.data_ptr(), f.scales.data_ptr(), y.data_ptr(), n, place.st);
+        rc = zccl_mx4_linear(x.t->data_ptr(), x.type, x.rows, x.cols, x.pitch, held.codes.data_ptr(), held.scales.data_ptr(), n, f.codes, f.scales, y.data_ptr(), n, place.st);
     return wrapped(rc, y);
 }
 
@@ -533,33 +558,33 @@ PyObject* mx4_linear_backward(PyObject*, Args a, Py_ssize_t na)
     Place place;
     if (!place.take(Py_None, *x.t)) return nullptr;
     at::Tensor dx, dw;
-    Form xl, xr, wl, wr;
-    zccl_mx4_job jobs[4];
-    int count = 0;
+    InnerForms inner;
     if (want_x) {
-        xl = new_form(m, n, *x.t);
-        xr = new_form(k, n, *x.t);
+        inner.add(m, n);
+        inner.add(k, n);
         dx = new_matrix(m, k, x.t->scalar_type(), *x.t);
-        jobs[count++] = dy.job(false, xl);
-        jobs[count++] = w.job(true, xr);
     }
     if (want_w) {
-        wl = new_form(n, m, *x.t);
-        wr = new_form(k, m, *x.t);
+        inner.add(n, m);
+        inner.add(k, m);
         dw = new_matrix(n, k, w.t->scalar_type(), *x.t);
-        jobs[count++] = dy.job(true, wl);
-        jobs[count++] = x.job(true, wr);
     }
+    inner.take(*x.t);
+    const struct { const Matrix* from; bool transpose, wanted; } operands[4] = {{&dy, false, want_x}, {&w, true, want_x}, {&dy, true, want_w}, {&x, true, want_w}};
+    zccl_mx4_job jobs[4];
+    int types[4], count = 0;
+    for (const auto& o : operands)
+        if (o.wanted) {
+            const Inner f = inner[count];
+            types[count] = o.from->type;
+            jobs[count++] = o.from->job(o.transpose, f.codes, f.scales);
+        }
     int rc = ZCCL_OK;
     if (dy.type == x.type && w.type == x.type) rc = zccl_mx4_quantize_all(jobs, count, x.type, place.st);
-    else {
-        if (want_x) rc = dy.quantize(false, xl, place.st);
-        if (want_x && rc == ZCCL_OK) rc = w.quantize(true, xr, place.st);
-        if (want_w && rc == ZCCL_OK) rc = dy.quantize(true, wl, place.st);
-        if (want_w && rc == ZCCL_OK) rc = x.quantize(true, wr, place.st);
-    }
-    if (want_x && rc == ZCCL_OK) rc = multiply(xl, m, xr, k, n, dx, place.st);
-    if (want_w && rc == ZCCL_OK) rc = multiply(wl, n, wr, k, m, dw, place.st);
+    else
+        for (int i = 0; i < count && rc == ZCCL_OK; ++i) rc = zccl_mx4_quantize_all(&jobs[i], 1, types[i], place.st);
+    if (want_x && rc == ZCCL_OK) rc = multiply(inner[0], m, inner[1], k, n, dx, place.st);
+    if (want_w && rc == ZCCL_OK) rc = multiply(inner[count - 2], n, inner[count - 1], k, m, dw, place.st);
     if (rc != ZCCL_OK) return PyLong_FromLong(rc);
     Py_INCREF(Py_None);
     Py_INCREF(Py_None);

@@ -162,19 +162,26 @@ __device__ __forceinline__ void quantize_one(const MxJob& job, uint32_t cta, Col
     else if constexpr (KIND == kMxColumns) quantize_columns<T, true>(job, cta, sh);
     else quantize_columns<T, false>(job, cta, sh);
 }
-// One matrix: a kernel for each way, of which rows need half the registers of columns.  Columns wait for memory, so they take as many CTAs to an SM as a few
-// spilled registers buy: whole pairs of 16-bit elements four (8192 x 8192 bf16: 26.7 us; three 28.1, two 34.1), the others three (16384 x 4097 bf16:
-// 45.9 us; four 63.3, two 55.5).
+// CTAs that an SM is to hold, which is what registers a kernel may have.  Columns wait for memory, so where there are many CTAs as many are resident as a
+// few spilled registers buy: with whole pairs of 16-bit elements four (8192 x 8192 bf16: 26.7 us; three 28.1, two 34.1), otherwise three (16384 x 4097 bf16: 45.9 us;
+// four 63.3, two 55.5).  Where all are resident at two to an SM anyhow nothing is spilled (777 x 1000: 3.0 us, with four 5.8).  Rows need half the registers.
 template <class T, MxKind KIND>
-__global__ void __launch_bounds__(kMxThreads, KIND < kMxColumns ? (sizeof(T) == 2 ? 6 : 4) : KIND == kMxColumns && sizeof(T) == 2 ? 4 : 3) mx_quantize_kernel(const __grid_constant__ MxJob job)
+constexpr int ctas_of(bool many) { return KIND < kMxColumns ? (sizeof(T) == 2 ? 6 : 4) : !many ? 2 : KIND == kMxColumns && sizeof(T) == 2 ? 4 : 3; }
+
+// One matrix: a kernel for each way.
+template <class T, MxKind KIND, bool MANY>
+__global__ void __launch_bounds__(kMxThreads, ctas_of<T, KIND>(MANY)) mx_quantize_kernel(const __grid_constant__ MxJob job)
 {
     __shared__ ColumnsShared sh;
     pdl_enter();
     quantize_one<T, KIND>(job, blockIdx.x, sh);
 }
-// Several: the small ones of a layer would each take as long as a launch.
-template <class T>
-__global__ void __launch_bounds__(kMxThreads, sizeof(T) == 2 ? 4 : 3) mx_quantize_all_kernel(const __grid_constant__ MxJobs jobs)
+// Several: the small ones of a layer would each take as long as a launch.  With rows alone a kernel that knows no columns, since two CTAs' worth of
+// registers would be too few warps for them (two of 4096 x 4096 bf16: 29 us at two CTAs to an SM, 19 at four).
+enum MxMix { kMxRowsAlone, kMxFewColumns, kMxManyColumns };
+template <class T, MxMix MIX>
+__global__ void __launch_bounds__(kMxThreads, MIX == kMxRowsAlone ? ctas_of<T, kMxRows>(true) : ctas_of<T, kMxColumns>(MIX == kMxManyColumns))
+mx_quantize_all_kernel(const __grid_constant__ MxJobs jobs)
 {
     __shared__ ColumnsShared sh;
     pdl_enter();
@@ -186,8 +193,11 @@ __global__ void __launch_bounds__(kMxThreads, sizeof(T) == 2 ? 4 : 3) mx_quantiz
         case kMxRowsStrips: quantize_one<T, kMxRowsStrips>(job, cta, sh); break;
         case kMxRows: quantize_one<T, kMxRows>(job, cta, sh); break;
         case kMxRowsPlain: quantize_one<T, kMxRowsPlain>(job, cta, sh); break;
-        case kMxColumns: quantize_one<T, kMxColumns>(job, cta, sh); break;
-        default: quantize_one<T, kMxColumnsPlain>(job, cta, sh); break;
+        default:
+            if constexpr (MIX != kMxRowsAlone) {
+                if (job.kind == kMxColumns) quantize_one<T, kMxColumns>(job, cta, sh);
+                else quantize_one<T, kMxColumnsPlain>(job, cta, sh);
+            }
     }
 }
 
@@ -313,7 +323,7 @@ int quantize_all(const zccl_mx4_job* jobs, int count, cudaStream_t st)
 {
     MxJobs list;
     for (int at = 0; at < count;) {
-        unsigned ctas = 0;
+        unsigned ctas = 0, columns = 0;
         list.count = 0;
         for (; at < count && list.count < kMxJobs; ++at) {
             if (jobs[at].rows == 0 || jobs[at].cols == 0) continue;
@@ -323,15 +333,23 @@ int quantize_all(const zccl_mx4_job* jobs, int count, cudaStream_t st)
             if (ctas > kMxMaxGroups - mine) break;
             job.first = ctas;
             ctas += mine;
+            if (job.kind >= kMxColumns) columns += mine;
             ++list.count;
         }
         if (list.count == 0) continue;
+        int dev = 0, sms = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return ZCCL_E_CUDA;
         int rc;
-        if (list.count > 1) rc = launched(launch_k(mx_quantize_all_kernel<T>, dim3(ctas), dim3(kMxThreads), 0, st, list));
+        const bool many = columns > (list.count > 1 ? 1u : 2u) * (unsigned)sms;   // several: rows' CTAs want room too
+        if (list.count > 1)
+            rc = launched(launch_k(columns == 0 ? mx_quantize_all_kernel<T, kMxRowsAlone> : many ? mx_quantize_all_kernel<T, kMxManyColumns> : mx_quantize_all_kernel<T, kMxFewColumns>,
+                                   dim3(ctas), dim3(kMxThreads), 0, st, list));
         else {
-            const auto kernel = list.job[0].kind == kMxRowsStrips ? mx_quantize_kernel<T, kMxRowsStrips> : list.job[0].kind == kMxRows ? mx_quantize_kernel<T, kMxRows>
-                                : list.job[0].kind == kMxRowsPlain ? mx_quantize_kernel<T, kMxRowsPlain> : list.job[0].kind == kMxColumns ? mx_quantize_kernel<T, kMxColumns>
-                                                                                                                                           : mx_quantize_kernel<T, kMxColumnsPlain>;
+            const MxKind kind = list.job[0].kind;
+            const auto kernel = kind == kMxRowsStrips ? mx_quantize_kernel<T, kMxRowsStrips, true> : kind == kMxRows ? mx_quantize_kernel<T, kMxRows, true>
+                                : kind == kMxRowsPlain ? mx_quantize_kernel<T, kMxRowsPlain, true>
+                                : kind == kMxColumns ? (many ? mx_quantize_kernel<T, kMxColumns, true> : mx_quantize_kernel<T, kMxColumns, false>)
+                                                     : (many ? mx_quantize_kernel<T, kMxColumnsPlain, true> : mx_quantize_kernel<T, kMxColumnsPlain, false>);
             rc = launched(launch_k(kernel, dim3(ctas), dim3(kMxThreads), 0, st, list.job[0]));
         }
         if (rc != ZCCL_OK) return rc;

@@ -53,11 +53,9 @@ def _value(r, what: str):
 def quantize(x: torch.Tensor, transpose: bool = False, out: Mx4 | None = None, stream=None) -> Mx4:
     """x (float32, bfloat16 or float16 [rows, cols], rows contiguous) in microscaled form, blocks along its rows; with
     `transpose` the form of x's transpose, blocks along x's columns."""
-    if x.dim() != 2:
-        raise ValueError("expected a matrix")
-    rows, cols = reversed(x.shape) if transpose else x.shape
     if out is None:
-        return Mx4(*_value(z.native().mx4_quantize(x, transpose, None, None, stream), "zccl_mx4_quantize"), rows, cols)
+        return Mx4._make(_value(z.native().mx4_quantize(x, transpose, None, None, stream), "zccl_mx4_quantize"))
+    rows, cols = reversed(x.shape) if transpose else x.shape
     if (out.rows, out.cols) != (rows, cols):
         raise ValueError(f"expected the form of a matrix [{rows}, {cols}], got one of [{out.rows}, {out.cols}]")
     _value(z.native().mx4_quantize(x, transpose, out.codes, out.scales, stream), "zccl_mx4_quantize")
