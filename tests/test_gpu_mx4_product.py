@@ -204,7 +204,7 @@ def test_gradient_against_differences(mx):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
-@pytest.mark.parametrize("m", [1, 2, 3, 5, 8, 9, 13, 16, 17, 70, 129])
+@pytest.mark.parametrize("m", [1, 2, 3, 5, 8, 9, 13, 16, 17, 40, 64, 65, 129])
 def test_a_layer_with_held_weights_is_quantising_and_multiplying(mx, m, dtype):
     """Few rows are quantised inside the product: the same bits, at every way in which the depth can end and for rows that begin anywhere."""
     for k, n in ((1, 20), (31, 200), (64, 129), (127, 300), (129, 1000), (257, 300), (1000, 500), (2049, 700), (4161, 3000), (8192, 4096), (20000, 300)):
