@@ -204,8 +204,8 @@ mx_quantize_all_kernel(const __grid_constant__ MxJobs jobs)
 // Back: 16 lanes take STRIP runs of 128 neighbouring elements of a row, a lane as many as make 16 bytes of the output at a time, so a store of the
 // 16 lanes is one run of whole sectors.  Rows that begin on 16 bytes (WIDE) have their runs begin there; elsewhere runs begin at the row's first 16-byte
 // boundary, `head` elements in, and a lane's elements are cut out of two words of codes and may lie in two blocks; the head and the end are stored one by one
-// (codes and scales are not __restrict__: the kernel in front may still be writing them, and loads of what never changes could be moved in front of the wait.)
-// (16384 x 4097 bf16: 59 us against 73.6 us one by one; 8192 x 8192, on boundaries: 27.5 us, 6.2 TB/s).
+// (16384 x 4097 bf16: 52 us against 73.6 us one by one; 8192 x 8192, on boundaries: 27.5 us, 6.2 TB/s).
+// Codes and scales are not __restrict__: the kernel in front may still be writing them, and loads of what never changes could be moved in front of the wait.
 template <class T, bool WIDE, int STRIP>
 __global__ void __launch_bounds__(kMxThreads) mx_dequantize_kernel(const uint32_t* codes, const unsigned char* scales, uint32_t rows,
                                                                     uint32_t cols, uint32_t blocks, uint32_t groups, uint32_t strips, uint32_t total, uint32_t step_row,
@@ -361,9 +361,10 @@ template <class T, bool VEC>
 cudaError_t launch_back(const void* codes, const void* scales, size_t rows, size_t cols, T* y, size_t pitch, cudaStream_t st)
 {
     const size_t blocks = mx_blocks(cols), groups = mx_groups(cols);
-    const bool four = strips_pay(rows, groups);
-    const Rounds k = rounds_of(rows, groups, four ? 4 : 1);
-    return launch_k(four ? mx_dequantize_kernel<T, VEC, 4> : mx_dequantize_kernel<T, VEC, 1>, dim3(k.ctas), dim3(kMxThreads), 0, st, (const uint32_t*)codes,
+    constexpr int kStrip = VEC && sizeof(T) == 2 ? 4 : 2;   // the others hold more for each run (8192 x 8192 to f32: 50.6 us, with four 55.2)
+    const bool many = strips_pay(rows, groups);
+    const Rounds k = rounds_of(rows, groups, many ? kStrip : 1);
+    return launch_k(many ? mx_dequantize_kernel<T, VEC, kStrip> : mx_dequantize_kernel<T, VEC, 1>, dim3(k.ctas), dim3(kMxThreads), 0, st, (const uint32_t*)codes,
                     (const unsigned char*)scales, (uint32_t)rows, (uint32_t)cols, (uint32_t)blocks, (uint32_t)groups, k.strips, k.total, k.step_row, k.step_strip, y, pitch);
 }
 
