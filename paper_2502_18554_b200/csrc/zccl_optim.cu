@@ -249,14 +249,41 @@ __device__ __forceinline__ void noise_of(uint32_t h, uint32_t& first, uint32_t& 
     second = prmt(h, 0, 0x4104) ^ first;
 }
 
+// Two neighbours as one operand: the multiplications and additions of two elements are one instruction, each rounded as it would be alone.
+struct Two { unsigned long long w; };
+__device__ __forceinline__ Two two(float a, float b)
+{
+    Two t;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(t.w) : "f"(a), "f"(b));
+    return t;
+}
+__device__ __forceinline__ void both(Two t, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(t.w)); }
+__device__ __forceinline__ Two times(Two a, Two b)
+{
+    Two t;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(t.w) : "l"(a.w), "l"(b.w));
+    return t;
+}
+__device__ __forceinline__ Two times_plus(Two a, Two b, Two c)
+{
+    Two t;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(t.w) : "l"(a.w), "l"(b.w), "l"(c.w));
+    return t;
+}
+// The largest of three, NaN where one of them is.
+__device__ __forceinline__ float largest(float a, float b, float c)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
 // The largest magnitude of a block, as bits, of which four neighbouring lanes hold eight each.
-template <bool ROOT>
 __device__ __forceinline__ uint32_t top8(const float (&v)[8])
 {
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, ROOT ? __float_as_uint(v[i]) : __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    if (ROOT) top &= 0x7FFFFFFFu;                    // roots are not negative; a NaN may have a sign
+    const float t = largest(fabsf(v[0]), fabsf(v[1]), fabsf(v[2]));
+    const float u = largest(fabsf(v[3]), fabsf(v[4]), fabsf(v[5]));
+    uint32_t top = __float_as_uint(largest(t, u, largest(fabsf(v[6]), fabsf(v[7]), 0.0f)));
     top = max(top, __shfl_xor_sync(kFull, top, 1));
     return max(top, __shfl_xor_sync(kFull, top, 2));
 }
@@ -310,9 +337,12 @@ __device__ __forceinline__ uint2 pack8(float (&v)[8], const uint32_t (&noise)[8]
     }
     const float inverse = __uint_as_float((134u - s) << 23);
     uint32_t z[8], least = 0xFFFFFFFFu;
+    float scaled[8];
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) both(times(two(v[i], v[i + 1]), two(inverse, inverse)), scaled[i], scaled[i + 1]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const uint32_t bits = __float_as_uint(v[i] * inverse);
+        const uint32_t bits = __float_as_uint(scaled[i]);
         z[i] = (bits << 4) + noise[i];
         if (ROOT) least = min(least, z[i]);
         else z[i] |= bits & 0x80000000u;
@@ -348,13 +378,19 @@ struct AdamRates {
 template <bool EIGHT>
 __device__ __forceinline__ void update8(const AdamCall& call, const AdamRates& k, float m_unit, float v_unit, const float (&g)[8], float (&p)[8], float (&m)[8], float (&v)[8], float (&r)[8])
 {
+    const Two gain1 = two(k.gain1, k.gain1), gain2 = two(k.gain2, k.gain2), m_units = two(m_unit, m_unit), v_units = two(v_unit, v_unit);
+    const Two root = two(k.root, k.root), eps = two(call.eps, call.eps), keep = two(k.keep, k.keep), rate = two(-k.rate, -k.rate);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        m[i] = __fmaf_rn(k.gain1, g[i], m_unit * m[i]);
-        const float u = k.gain2 * g[i], w = v_unit * v[i];
-        v[i] = __fmaf_rn(u, u, EIGHT ? w * w : w);
+    for (int i = 0; i < 8; i += 2) {
+        const Two gi = two(g[i], g[i + 1]), u = times(gain2, gi), w = times(v_units, two(v[i], v[i + 1]));
+        const Two mi = times_plus(gain1, gi, times(m_units, two(m[i], m[i + 1])));
+        both(mi, m[i], m[i + 1]);
+        both(times_plus(u, u, EIGHT ? times(w, w) : w), v[i], v[i + 1]);
         r[i] = root_of(v[i]);
-        p[i] = __fmaf_rn(-k.rate, m[i] * reciprocal_of(__fmaf_rn(r[i], k.root, call.eps)), p[i] * k.keep);
+        r[i + 1] = root_of(v[i + 1]);
+        float d0, d1;
+        both(times_plus(two(r[i], r[i + 1]), root, eps), d0, d1);
+        both(times_plus(rate, times(mi, two(reciprocal_of(d0), reciprocal_of(d1))), times(two(p[i], p[i + 1]), keep)), p[i], p[i + 1]);
     }
 }
 // New states of eight elements to codes; `place` counts the first one.
@@ -364,8 +400,8 @@ __device__ __forceinline__ void encode_states(const AdamRates& k, unsigned long 
     uint32_t first[8], second[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) noise_of(random_bits((uint32_t)from ^ i, (uint32_t)(from >> 32)), first[i], second[i]);
-    ms = exponent8(top8<false>(m));
-    vs = exponent8(top8<true>(r));
+    ms = exponent8(top8(m));
+    vs = exponent8(top8(r));
     mc = pack8<false>(m, first, ms);
     vc = pack8<true>(r, second, vs);
 }
@@ -373,7 +409,8 @@ __device__ __forceinline__ void encode_states(const AdamRates& k, unsigned long 
 // A CTA takes a chunk of `passes` times 2048 elements of one tensor, a thread eight neighbours at a time.  Passes that are whole, of arrays on
 // 16-byte boundaries, go the short way, where the next eight are loaded while these are worked on.  States in 32 bits: bound by memory, two CTAs to an SM
 // have enough loads in flight.  In 8 bits: about 50 instructions to an element against 10 bytes, so issue and memory take about as long and warps have
-// to cover each other's waits: four CTAs, though a few registers are spilled for it (128 Mi bf16 parameters: 261 us, with two or three CTAs 335).
+// to cover each other's waits: four CTAs, though for binary32 a few registers are spilled for it (128 Mi bf16 parameters: 239 us; 261 us with every
+// multiplication an instruction of its own, and of those 335 with two or three CTAs).
 template <class P, class G, bool EIGHT, int CAP>
 __global__ void __launch_bounds__(kOptThreads, EIGHT ? 4 : 2) adamw_kernel(const __grid_constant__ AdamList<CAP> list, const __grid_constant__ AdamCall call)
 {
@@ -703,6 +740,7 @@ int zccl_adamw(const zccl_adamw_tensor* tensors, size_t count, const zccl_adamw_
     // them 128 Mi parameters with states in 8 bits took 298 us instead of 280, with eight 64 Mi with 32 bits 326 instead of 317: more is left at the end).
     call.passes = 1;
     while (call.passes < 4 && total / kPass > (size_t)kChunksWanted * call.passes) call.passes *= 2;
+    if (k.state_bits == 8 && total / kPass >= (size_t)32 * kChunksWanted) call.passes = 8;   // fewer starts: 128 Mi 266 us to 257 us; in 32 bits 64 Mi 317 us to 328 us
     return used <= (size_t)kFewTensors ? run_list<kFewTensors>(tensors, count, k, call, (cudaStream_t)stream)
                                        : run_list<kManyTensors>(tensors, count, k, call, (cudaStream_t)stream);
 }
