@@ -16,8 +16,8 @@ constexpr int kPass = kOptThreads * kPerThread;
 constexpr int kChunk = 4 * kPass;                   // elements of a gradient that a CTA takes the norm of at a time
 constexpr int kChunksWanted = 1024;                 // of a step, before they get longer
 // Tensors travel as kernel arguments, so a call copies nothing, needs no memory and can be captured.  Arguments above 4 KB cost
-// the launch a few microseconds, hence two sizes of the list.
-constexpr int kFewTensors = 40, kManyTensors = 360;
+// the launch a few microseconds, hence three sizes of the list (a step of 41 tensors 6.5 us on the host, with two sizes 11.4; of 100 12.6 and 14.5).
+constexpr int kFewTensors = 40, kMoreTensors = 128, kManyTensors = 360;
 
 // Which tensor chunk `c` belongs to: the last one that begins at or in front of it (tensors without elements have no chunks).
 template <class L>
@@ -741,8 +741,9 @@ int zccl_adamw(const zccl_adamw_tensor* tensors, size_t count, const zccl_adamw_
     call.passes = 1;
     while (call.passes < 4 && total / kPass > (size_t)kChunksWanted * call.passes) call.passes *= 2;
     if (k.state_bits == 8 && total / kPass >= (size_t)32 * kChunksWanted) call.passes = 8;   // fewer starts: 128 Mi 266 us to 257 us; in 32 bits 64 Mi 317 us to 328 us
-    return used <= (size_t)kFewTensors ? run_list<kFewTensors>(tensors, count, k, call, (cudaStream_t)stream)
-                                       : run_list<kManyTensors>(tensors, count, k, call, (cudaStream_t)stream);
+    if (used <= (size_t)kFewTensors) return run_list<kFewTensors>(tensors, count, k, call, (cudaStream_t)stream);
+    if (used <= (size_t)kMoreTensors) return run_list<kMoreTensors>(tensors, count, k, call, (cudaStream_t)stream);
+    return run_list<kManyTensors>(tensors, count, k, call, (cudaStream_t)stream);
 }
 
 size_t zccl_grad_norm_work(size_t count) { return (count / kFewTensors + 2) * kNormCtas * sizeof(double); }

@@ -135,7 +135,7 @@ def test_tensors_that_begin_anywhere(optim, bits, shift):
     check(s, before, HYPER, bits, seed=3)
 
 
-@pytest.mark.parametrize("count", [40, 41, 42, 364, 365, 380, 381, 1000])
+@pytest.mark.parametrize("count", [40, 41, 42, 129, 130, 132, 133, 364, 365, 380, 381, 1000])
 def test_many_tensors(optim, count):
     """The numbers of tensors around which the list's form and the number of launches change."""
     sizes = [(7 * i) % 97 for i in range(count - 1)] + [20_000]
@@ -216,6 +216,19 @@ def test_offsets_beyond_32_bits(optim):
         off = np.count_nonzero(got != want * np.repeat(np.ldexp(1.0, scale - 127), 32)[:tail])
         assert off <= 2      # see check(): a chance of 2^-15 per element
     assert not s["p"][1][:1 << 20].any() and not s["m"][1][1 << 31:(1 << 31) + (1 << 20)].view(torch.uint8).any()
+
+
+def test_a_step_of_many_elements_is_that_of_few(optim):
+    """How elements are divided among CTAs depends on how many there are in all; what becomes of a tensor does not."""
+    n, more = 9_000_011, (1 << 26) - 9_000_011
+    make = lambda: tensors([n], torch.bfloat16, torch.bfloat16, 8, seed=5)  # noqa: E731
+    s, twin = make(), make()
+    run(optim, s, seed=2)
+    other = {key: torch.zeros(more, dtype=x[0].dtype, device="cuda") for key, x in twin.items() if key in ("p", "g", "m", "v")}
+    other |= {key: torch.zeros(-(-more // 32), dtype=torch.uint8, device="cuda") for key in ("ms", "vs")}
+    run(optim, {key: x + [other[key]] for key, x in twin.items() if key in other}, seed=2)
+    for key in other:
+        assert torch.equal(s[key][0].view(torch.uint8), twin[key][0].view(torch.uint8)), key
 
 
 def test_a_gradient_that_is_not_finite_stays_in_its_block(optim):
