@@ -66,16 +66,21 @@ __device__ __forceinline__ uint32_t mx_encode8(const float (&v)[8])
 template <class T> struct MxTwo { uint32_t w; };
 template <> struct MxTwo<float> { float a, b; };
 
-// Largest magnitudes so far of the two places, as bits: magnitudes of floats are in the order of their bits, with infinity and
-// NaN at the top, so 16-bit types are compared as two halves of a word.
+// Largest magnitudes so far of the two places, as bits: a NaN stays, above infinity.
 template <class T> struct MxTop { uint32_t w = 0; };
-template <> struct MxTop<float> { uint32_t a = 0, b = 0; };
-template <class T>
-__device__ __forceinline__ void mx_top(MxTop<T>& top, const MxTwo<T>& v) { top.w = __vmaxu2(top.w, v.w & 0x7FFF7FFFu); }
+template <> struct MxTop<float> { float a = 0.0f, b = 0.0f; };
+__device__ __forceinline__ void mx_top(MxTop<__nv_bfloat16>& top, const MxTwo<__nv_bfloat16>& v)
+{
+    asm("{\n\t.reg .b32 a;\n\tabs.bf16x2 a, %1;\n\tmax.NaN.bf16x2 %0, %0, a;\n\t}" : "+r"(top.w) : "r"(v.w));
+}
+__device__ __forceinline__ void mx_top(MxTop<__half>& top, const MxTwo<__half>& v)
+{
+    asm("{\n\t.reg .b32 a;\n\tabs.f16x2 a, %1;\n\tmax.NaN.f16x2 %0, %0, a;\n\t}" : "+r"(top.w) : "r"(v.w));
+}
 __device__ __forceinline__ void mx_top(MxTop<float>& top, const MxTwo<float>& v)
 {
-    top.a = max(top.a, __float_as_uint(v.a) & 0x7FFFFFFFu);
-    top.b = max(top.b, __float_as_uint(v.b) & 0x7FFFFFFFu);
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(top.a) : "f"(fabsf(v.a)));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(top.b) : "f"(fabsf(v.b)));
 }
 // The bits of a magnitude in binary32.
 template <class T> __device__ __forceinline__ uint32_t mx_bits(uint32_t half);
@@ -83,8 +88,8 @@ template <> __device__ __forceinline__ uint32_t mx_bits<__nv_bfloat16>(uint32_t 
 template <> __device__ __forceinline__ uint32_t mx_bits<__half>(uint32_t half) { return __float_as_uint(__half2float(__ushort_as_half((unsigned short)half))); }
 template <class T> __device__ __forceinline__ uint32_t mx_first(const MxTop<T>& top) { return mx_bits<T>(top.w & 0xFFFFu); }
 template <class T> __device__ __forceinline__ uint32_t mx_second(const MxTop<T>& top) { return mx_bits<T>(top.w >> 16); }
-__device__ __forceinline__ uint32_t mx_first(const MxTop<float>& top) { return top.a; }
-__device__ __forceinline__ uint32_t mx_second(const MxTop<float>& top) { return top.b; }
+__device__ __forceinline__ uint32_t mx_first(const MxTop<float>& top) { return __float_as_uint(top.a); }
+__device__ __forceinline__ uint32_t mx_second(const MxTop<float>& top) { return __float_as_uint(top.b); }
 
 // Both elements times their powers of two, exactly, as binary32.  bfloat16 has binary32's exponents, so there the product of two elements is
 // one instruction (what falls below its range is far below the smallest code's half).
@@ -152,9 +157,9 @@ __device__ __forceinline__ void mx_decode8(uint32_t w, float (&v)[8])
     }
 }
 
-// Sixteen lanes' run of 128 elements, eight to a lane: the lane's codes, and in `four` the run's four biased exponents as a word (every lane's).
+// Four lanes' block, eight elements to a lane: the lane's codes, and the block's biased exponent.
 template <class T>
-__device__ __forceinline__ uint32_t quantize_run(const MxTwo<T> (&v)[4], uint32_t sub, uint32_t& four)
+__device__ __forceinline__ uint32_t quantize_block(const MxTwo<T> (&v)[4], uint32_t& s)
 {
     MxTop<T> two;
 #pragma unroll
@@ -162,16 +167,24 @@ __device__ __forceinline__ uint32_t quantize_run(const MxTwo<T> (&v)[4], uint32_
     uint32_t top = max(mx_first(two), mx_second(two));
     top = max(top, __shfl_xor_sync(kFull, top, 1));
     top = max(top, __shfl_xor_sync(kFull, top, 2));
-    const uint32_t s = mx_exponent(top);
+    s = mx_exponent(top);
     const float inverse = mx_inverse(s);
     const uint32_t both = mx_pair(inverse, inverse);
     float f[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) mx_scaled(v[i], inverse, inverse, both, f[2 * i], f[2 * i + 1]);
+    return s == 255u ? 0u : mx_encode8(f);
+}
+// Sixteen lanes' run of 128 elements: the lane's codes, and in `four` the run's four biased exponents as a word (every lane's).
+template <class T>
+__device__ __forceinline__ uint32_t quantize_run(const MxTwo<T> (&v)[4], uint32_t sub, uint32_t& four)
+{
+    uint32_t s;
+    const uint32_t w = quantize_block(v, s);
     four = s << (8 * (sub >> 2));
     four |= __shfl_xor_sync(kFull, four, 4);
     four |= __shfl_xor_sync(kFull, four, 8);
-    return s == 255u ? 0u : mx_encode8(f);
+    return w;
 }
 
 }  // namespace

@@ -736,11 +736,11 @@ int zccl_adamw(const zccl_adamw_tensor* tensors, size_t count, const zccl_adamw_
     call.norm = k.norm;
     call.max_norm = (float)k.max_norm;
     call.copy_type = k.copy_type;
-    // Small models are spread over the SMs; large ones have chunks of four passes, whose first loads alone are not covered by work (with two of
-    // them 128 Mi parameters with states in 8 bits took 298 us instead of 280, with eight 64 Mi with 32 bits 326 instead of 317: more is left at the end).
+    // Small models are spread over the SMs; large ones have chunks of several passes, whose first loads alone are not covered by work.  Of two, four and eight
+    // passes 64 Mi parameters with states in 32 bits took 326, 317 and 328 us (more is left at the end), 128 Mi with 8 bits 285, 266 and 257.
     call.passes = 1;
     while (call.passes < 4 && total / kPass > (size_t)kChunksWanted * call.passes) call.passes *= 2;
-    if (k.state_bits == 8 && total / kPass >= (size_t)32 * kChunksWanted) call.passes = 8;   // fewer starts: 128 Mi 266 us to 257 us; in 32 bits 64 Mi 317 us to 328 us
+    if (k.state_bits == 8 && total / kPass >= (size_t)32 * kChunksWanted) call.passes = 8;
     if (used <= (size_t)kFewTensors) return run_list<kFewTensors>(tensors, count, k, call, (cudaStream_t)stream);
     if (used <= (size_t)kMoreTensors) return run_list<kMoreTensors>(tensors, count, k, call, (cudaStream_t)stream);
     return run_list<kManyTensors>(tensors, count, k, call, (cudaStream_t)stream);
