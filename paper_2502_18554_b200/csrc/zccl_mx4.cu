@@ -31,9 +31,9 @@ struct MxJobs {
 // Rows: 16 lanes take STRIP groups of 128 neighbouring elements of a row (a group: four blocks, one word of scales), a lane
 // eight elements of each, so loads are 16 bytes a lane and codes leave as whole lines.  Blocks behind the last are quantised as zeros. CTAs from
 // `work` on write the scales of the rows that fill the last band up, a word a thread.
-// Bound by memory where it is large (8192 x 8192 bf16: 27.2 us, 6.2 TB/s; a byte of scale from every fourth lane, 28.2 us where a lane puts four together); with one group at a time the indexes cost more instructions than the elements
-// (23 to an element, 52.5 us).  Rows that do not begin on 16-byte boundaries are loaded element by element and take twice as long (16384 x 4097: 57 us; cutting them out
-// of aligned pieces took as long).
+// Bound by memory where it is large (8192 x 8192 bf16: 25.8 us, 6.6 TB/s); with one group at a time the indexes cost more instructions than the elements
+// (23 to an element, 52.5 us).  The lane that has a block's scale stores it: putting four together for one lane to store took 3 % longer.  Rows that do not begin on
+// 16-byte boundaries are loaded element by element and take twice as long (16384 x 4097: 56 us; cutting them out of aligned pieces took as long).
 template <class T, bool VEC, int STRIP>
 __device__ __forceinline__ void quantize_rows(const MxJob& job, uint32_t cta)
 {
@@ -163,7 +163,7 @@ __device__ __forceinline__ void quantize_one(const MxJob& job, uint32_t cta, Col
     else quantize_columns<T, false>(job, cta, sh);
 }
 // CTAs that an SM is to hold, which is what registers a kernel may have.  Columns wait for memory, so where there are many CTAs as many are resident as a
-// few spilled registers buy: with whole pairs of 16-bit elements four (8192 x 8192 bf16: 26.7 us; three 28.1, two 34.1), otherwise three (16384 x 4097 bf16: 45.9 us;
+// few spilled registers buy: with whole pairs of 16-bit elements four (8192 x 8192 bf16: 26.4 us; three 28.1, two 34.1), otherwise three (16384 x 4097 bf16: 42.9 us;
 // four 63.3, two 55.5).  Where all are resident at two to an SM anyhow nothing is spilled (777 x 1000: 3.0 us, with four 5.8).  Rows need half the registers.
 template <class T, MxKind KIND>
 constexpr int ctas_of(bool many) { return KIND < kMxColumns ? (sizeof(T) == 2 ? 6 : 4) : !many ? 2 : KIND == kMxColumns && sizeof(T) == 2 ? 4 : 3; }

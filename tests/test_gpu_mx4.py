@@ -98,6 +98,17 @@ def test_every_half_value_lands_where_the_formula_says(mx):
 
 
 @pytest.mark.parametrize("transpose", [False, True])
+@pytest.mark.parametrize("top", [0.0, 2.0 ** -133, 2.0 ** -126, 1.0, 1.5 * 2.0 ** 127])
+def test_every_bfloat16_lands_where_the_formula_says(mx, top, transpose):
+    """Every pattern of 16 bits, infinities and NaN among them, next to numbers from the smallest to the largest binade."""
+    bits = torch.arange(0, 1 << 16, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    x = torch.zeros(bits.numel(), 32, dtype=torch.bfloat16)
+    x[:, 0], x[:, 30] = bits, top
+    x = x.t().contiguous() if transpose else x
+    check(mx, x, transpose, mx.quantize(x.cuda(), transpose=transpose))
+
+
+@pytest.mark.parametrize("transpose", [False, True])
 def test_a_large_matrix(mx, transpose):
     """Sizes at which warps go round several times, against the same formula on the GPU in 64 bits (torch)."""
     x = torch.randn(16385, 4097, device="cuda", dtype=torch.bfloat16)
