@@ -51,6 +51,16 @@ __device__ __forceinline__ bool wait_for_cluster(unsigned long long* bar, uint32
     atomicOr(&g_product_status, kStuck);
     return false;
 }
+// The loading thread's last act: what it has asked for (n stages' worth, `loads`: at this CTA's barriers) lands, and what the tensor core still arrives for at
+// `empty` has arrived, before the memory is given up, whether it is used or not.  `ok`: no wait has run out so far; after one the issuing thread may have given up.
+template <int STAGES>
+__device__ __forceinline__ void settle(unsigned long long* full, unsigned long long* empty, uint32_t n, bool loads, bool ok)
+{
+    for (uint32_t i = n < (uint32_t)STAGES ? 0 : n - STAGES; i < n; ++i) {
+        if (loads) ok &= wait_for(&full[i % STAGES], (i / STAGES) & 1);
+        ok = ok && wait_for(&empty[i % STAGES], (i / STAGES) & 1);
+    }
+}
 __device__ __forceinline__ unsigned char* on_1024(unsigned char* raw) { return raw + (1024 - (smem_u32(raw) & 1023u)) % 1024; }
 
 // How much of the contraction is left from depth tile k on, in groups of 128 (0, 1 or 2) and instructions (up to 4).
@@ -283,16 +293,16 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
     if (warp == 0) {
         if (loads) {
             uint32_t n = 0;
+            bool ok = true;
             for (uint32_t d = k_begin; d < k_end; ++d, ++n) {
                 const uint32_t s = n % kStages;
-                if (n >= kStages && !wait_for(&empty[s], (n / kStages - 1) & 1)) break;
+                if (n >= kStages && !(ok = wait_for(&empty[s], (n / kStages - 1) & 1))) break;
                 if (n >= asked) load_rows(s, d);
                 unsigned char* const at = tiles + s * S::kStage;
                 tile_load(at + S::kColAt, &c_map, (int)(d * kRowBytes), (int)c0, &full[s]);
                 bytes_load(at + S::kColScaleAt, k.c_scales + ((size_t)(c0 / kMxBand) * groups + 2 * d) * kMxTileBytes, groups_at(d, k.depth_blocks) * kMxTileBytes, &full[s]);
             }
-            // what has been asked for lands before the memory is given up, whether it is used or not
-            for (uint32_t i = n < kStages ? 0 : n - kStages; i < n; ++i) wait_for(&full[i % kStages], (i / kStages) & 1);
+            settle<kStages>(full, empty, n, true, ok);
         }
     } else if (warp == 1) {
         if (elect_one()) {
@@ -356,6 +366,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
     }
     __syncwarp();
     cluster_sync();                        // nobody leaves while its sums are still read
+    tcgen05_fence_after();
     if (warp == 1) tmem_free(tmem, S::kColumns);
 }
 
@@ -466,11 +477,12 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_token_kernel(const __g
     if (warp == 0) {
         if (lane == 0) {
             uint32_t n = asked;
+            bool ok = true;
             for (; n < mine; ++n) {
-                if (n >= (uint32_t)kStages && !wait_for(&empty[n % kStages], (n / kStages - 1) & 1)) break;
+                if (n >= (uint32_t)kStages && !(ok = wait_for(&empty[n % kStages], (n / kStages - 1) & 1))) break;
                 load(n);
             }
-            for (uint32_t i = n < (uint32_t)kStages ? 0 : n - kStages; i < n; ++i) wait_for(&full[i % kStages], (i / kStages) & 1);
+            settle<kStages>(full, empty, n, true, ok);
         }
     } else if (warp == 1) {
         if (elect_one()) {
@@ -514,6 +526,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_token_kernel(const __g
     }
     __syncwarp();
     cluster_sync();                        // nobody leaves while its sums are still read
+    tcgen05_fence_after();
     if (warp == 1) tmem_free(tmem, S::S::kColumns);
 }
 
@@ -596,9 +609,7 @@ __global__ void __launch_bounds__(PairShape::kThreads, 1) mx4_pair_kernel(const 
                     scales_load_pair(at + S::kColScaleAt, &c_scale_map, (int)(2 * d), (int)(ct * S::kBands), bar);
                 }
             }
-            // what has been asked for lands before the memory is given up, whether it is used or not: the first CTA sees all of it
-            if (rank == 0)
-                for (uint32_t i = n < kStages ? 0 : n - kStages; i < n; ++i) wait_for(&full[i % kStages], (i / kStages) & 1);
+            settle<kStages>(full, empty, n, rank == 0, ok);   // the first CTA sees both's loads; each sees the arrivals at its own `empty`
         }
     } else if (warp == 1) {
         if (rank == 0 && elect_one()) {
@@ -642,7 +653,7 @@ __global__ void __launch_bounds__(PairShape::kThreads, 1) mx4_pair_kernel(const 
                 }
                 tcgen05_commit_pair(&done);
             }
-            tcgen05_commit_pair(&drained);
+            tcgen05_commit_own(&drained);
             wait_for(&drained, 0);
         }
     } else {
@@ -663,7 +674,9 @@ __global__ void __launch_bounds__(PairShape::kThreads, 1) mx4_pair_kernel(const 
     }
     __syncwarp();
     tcgen05_fence_before();
-    cluster_sync();                        // neither leaves while the other still reaches its barriers or its tensor memory
+    // Neither leaves while the other still reaches its barriers or its tensor memory.  The tensor core's arrivals at the second CTA's barriers are no thread's
+    // doing and not ordered by this: that CTA has waited for each of them itself (`done` where sums are read out, `empty` in settle).
+    cluster_sync();
     tcgen05_fence_after();
     if (warp == 1) tmem_free_pair(tmem, S::kColumns);
 }

@@ -111,6 +111,11 @@ __device__ __forceinline__ void tcgen05_commit_pair(unsigned long long* bar)
 {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)), "h"((unsigned short)3) : "memory");
 }
+// The same at this CTA's barrier alone.
+__device__ __forceinline__ void tcgen05_commit_own(unsigned long long* bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 __device__ __forceinline__ void tcgen05_copy_scales_pair(uint32_t column, unsigned long long descriptor)
 {
     asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(column), "l"(descriptor) : "memory");

@@ -261,3 +261,37 @@ def test_leading_dimensions_and_refusals(mx):
     with pytest.raises(RuntimeError):
         big = torch.zeros(q.codes.numel() + 8, dtype=torch.uint8, device="cuda")
         mx.matmul(mx.Mx4(big[8:], q.scales, 40, 64), q)
+
+
+def test_pairs_of_ctas_that_follow_each_other(mx):
+    """Short products of many tiles on several streams, so that one's CTAs take the places (shared and tensor memory, barriers) that another's have just left; every
+    round's outputs are compared."""
+    shapes = [(4096, 4096, 64), (4097, 3900, 300), (2600, 2600, 1300), (128, 20000, 256), (6000, 6001, 32)]
+    work = []
+    for i, (m, n, k) in enumerate(shapes):
+        a, b = operand(m, k, i), operand(n, k, i + 50)
+        work.append((mx.Mx4(a[0], a[1], m, k), mx.Mx4(b[0], b[1], n, k)))
+    want = [mx.matmul(a, b) for a, b in work]
+    streams = [torch.cuda.Stream() for _ in work]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        got = [[mx.matmul(a, b, stream=s) for _ in range(3)] for (a, b), s in zip(work, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, ys in zip(want, got) for y in ys)
+    assert mx.status() == 0
+
+
+def test_every_round_of_products_on_several_streams(mx):
+    """Kernels of every form side by side, each round's outputs compared."""
+    shapes = [(1, 4096, 4096), (64, 4096, 4096), (128, 3000, 5000), (1500, 1500, 2048), (4096, 4096, 512), (200, 200, 8192)]
+    work = []
+    for i, (m, n, k) in enumerate(shapes):
+        a, b = operand(m, k, i), operand(n, k, i + 50)
+        work.append((mx.Mx4(a[0], a[1], m, k), mx.Mx4(b[0], b[1], n, k)))
+    want = [mx.matmul(a, b, torch.float32) for a, b in work]
+    streams = [torch.cuda.Stream() for _ in work]
+    torch.cuda.synchronize()
+    rounds = [[mx.matmul(a, b, torch.float32, stream=s) for (a, b), s in zip(work, streams)] for _ in range(20)]
+    torch.cuda.synchronize()
+    assert mx.status() == 0
+    assert all(torch.equal(x, y) for got in rounds for x, y in zip(want, got))
