@@ -28,6 +28,8 @@ struct MxJobs {
     int count;
 };
 
+// Inputs are not __restrict__ anywhere here: the kernel in front may still be writing them, and loads of what never changes could be moved in front of the wait.
+
 // Rows: 16 lanes take STRIP groups of 128 neighbouring elements of a row (a group: four blocks, one word of scales), a lane
 // eight elements of each, so loads are 16 bytes a lane and codes leave as whole lines.  Blocks behind the last are quantised as zeros. CTAs from
 // `work` on write the scales of the rows that fill the last band up, a word a thread.
@@ -37,7 +39,7 @@ struct MxJobs {
 template <class T, bool VEC, int STRIP>
 __device__ __forceinline__ void quantize_rows(const MxJob& job, uint32_t cta)
 {
-    const T* __restrict__ const x = (const T*)job.x;
+    const T* const x = (const T*)job.x;
     const uint32_t rows = job.rows, cols = job.cols, blocks = job.blocks, groups = job.groups, strips = job.strips, total = job.total, work = job.work;
     const uint32_t step_row = job.step_row, step_strip = job.step_strip;
     const size_t pitch = job.pitch;
@@ -94,7 +96,7 @@ struct ColumnsShared {
 template <class T, bool VEC>
 __device__ __forceinline__ void quantize_columns(const MxJob& job, uint32_t cta, ColumnsShared& sh)
 {
-    const T* __restrict__ const x = (const T*)job.x;
+    const T* const x = (const T*)job.x;
     const uint32_t rows = job.rows, cols = job.cols, blocks = job.blocks, groups = job.groups, across = job.across;
     const size_t pitch = job.pitch;
     uint4* __restrict__ const codes = (uint4*)job.codes;
@@ -205,7 +207,6 @@ mx_quantize_all_kernel(const __grid_constant__ MxJobs jobs)
 // 16 lanes is one run of whole sectors.  Rows that begin on 16 bytes (WIDE) have their runs begin there; elsewhere runs begin at the row's first 16-byte
 // boundary, `head` elements in, and a lane's elements are cut out of two words of codes and may lie in two blocks; the head and the end are stored one by one
 // (16384 x 4097 bf16: 52 us against 73.6 us one by one; 8192 x 8192, on boundaries: 27.5 us, 6.2 TB/s).
-// Codes and scales are not __restrict__: the kernel in front may still be writing them, and loads of what never changes could be moved in front of the wait.
 template <class T, bool WIDE, int STRIP>
 __global__ void __launch_bounds__(kMxThreads) mx_dequantize_kernel(const uint32_t* codes, const unsigned char* scales, uint32_t rows,
                                                                     uint32_t cols, uint32_t blocks, uint32_t groups, uint32_t strips, uint32_t total, uint32_t step_row,

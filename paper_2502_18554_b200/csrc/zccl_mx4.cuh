@@ -113,9 +113,9 @@ __device__ __forceinline__ void mx_scaled(const MxTwo<__nv_bfloat16>& v, float, 
 // 2^-e of two places as a pair of bfloat16.
 __device__ __forceinline__ uint32_t mx_pair(float first, float second) { return __float_as_uint(first) >> 16 | (__float_as_uint(second) & 0xFFFF0000u); }
 
-// Eight neighbouring elements of a row; what lies behind `cols` counts as zero.
+// Eight neighbouring elements of a row; what lies behind `cols` counts as zero.  The row is not __restrict__ (see zccl_mx4.cu).
 template <class T, bool VEC>
-__device__ __forceinline__ void load8(const T* __restrict__ row, uint32_t at, uint32_t cols, MxTwo<T> (&v)[4])
+__device__ __forceinline__ void load8(const T* row, uint32_t at, uint32_t cols, MxTwo<T> (&v)[4])
 {
     if (VEC && at + 8 <= cols) {
 #pragma unroll

@@ -295,3 +295,32 @@ def test_every_round_of_products_on_several_streams(mx):
     torch.cuda.synchronize()
     assert mx.status() == 0
     assert all(torch.equal(x, y) for got in rounds for x, y in zip(want, got))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_calls_that_read_what_the_call_in_front_writes(mx, dtype):
+    """Products, forms along rows and columns, the way back and layers one behind the other without a synchronisation, each reading what the kernel in front has
+    just written; inputs change from round to round, so that what is left from the last round would show."""
+    gen = torch.Generator().manual_seed(11)
+    for m, k, n in ((5, 300, 260), (300, 260, 512), (1500, 1100, 900)):
+        w = mx.quantize((torch.randn(k, n, generator=gen) * 0.1).to(dtype).cuda(), transpose=True)      # [n, k]
+        back = mx.quantize((torch.randn(k, n, generator=gen) * 0.1).to(dtype).cuda())                   # [k, n]
+        xs = [torch.randn(m, k, generator=gen).to(dtype).cuda() for _ in range(6)]
+
+        def chain(x, settle):
+            out = []
+            for _ in range(3):
+                steps = [lambda a: mx.quantize(a), lambda a: mx.matmul(a, w, dtype), lambda a: mx.quantize(a, transpose=True), lambda a: mx.dequantize(a, dtype).t().contiguous(),
+                         lambda a: mx.linear(a, back)]
+                for step in steps:
+                    x = step(x)
+                    if settle:
+                        torch.cuda.synchronize()
+                    out += [x.codes, x.scales] if isinstance(x, mx.Mx4) else [x]
+            return out
+
+        want = [chain(x, True) for x in xs]
+        got = [chain(x, False) for x in xs]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for p, q in zip(want, got) for a, b in zip(p, q))
+    assert mx.status() == 0
