@@ -1,13 +1,17 @@
 """What a data-parallel program does with the gradient that the ring has reduced: the norm over all tensors and the AdamW
 step over all of them at once, states in 32 or in 8 bits (``zccl_grad_norm`` and ``zccl_adamw`` in ``include/zccl.h``, which
-state the arithmetic).  Calls only enqueue on the stream; there is no CPU fallback.
+state the arithmetic).  Calls only enqueue on the stream, but for an exchange, which waits; there is no CPU fallback.
 """
 from __future__ import annotations
 
+import math
+
+import numpy as np
 import torch
 
 from . import zccl as z
 from .mx import _value
+from .ring import DegenerateRange
 
 BLOCK = 32
 
@@ -31,20 +35,80 @@ def adamw(params, grads, exp_avg, exp_avg_sq, exp_avg_scale=None, exp_avg_sq_sca
 
 
 def exchange(ring, grads, eb_mode: int, eb: float) -> list[torch.Tensor]:
-    """The gradients' average over the ranks of `ring` (a `ring.Ring`), compressed on the way: one Allreduce of all of them, as float32, in
-    which every rank ends with the same values (ZCCL_CONSISTENT_OWNER).  Returns tensors of the gradients' shapes, views of one array in which each
-    begins at a multiple of 32 elements; the gaps hold zeros, which count into the range that a relative bound refers to."""
-    at, spans, grads = 0, [], list(grads)
-    if not grads:
-        return []
+    """The gradients' average over the ranks of `ring` (a `ring.Ring` for at least exchange_elems(grads) elements), compressed on the way: one Allreduce of all of
+    them, as float32, in which every rank ends with the same values (ZCCL_CONSISTENT_OWNER).  Returns tensors of the gradients' shapes, views of one array in which
+    each begins at a multiple of 32 elements; the gaps hold zeros, which count into the range that a relative bound refers to.
+
+    The codec takes finite values only, so the ranks agree on the smallest and largest value of all gradients first (the host waits for it).  Where a gradient of any
+    rank is not finite, what is returned is NaN throughout, on every rank.  Where all values of all ranks are one, it is returned as it is.  An exchange that a rank has to
+    refuse (values beyond 2^30 steps of the bound, a range that is not finite) raises on every rank."""
+    return _exchange(ring, list(grads), eb_mode, eb)[0]
+
+
+def exchange_elems(grads) -> int:
+    """Elements of the array that `exchange` sends: what its ring has to be made for."""
+    return sum(-(-g.numel() // BLOCK) * BLOCK for g in grads)
+
+
+def _exchange(ring, grads: list, eb_mode: int, eb: float):
+    """(exchange's tensors, whether all gradients of all ranks are finite)."""
+    at, spans = 0, []
     for g in grads:
         spans.append((at, g.numel()))
         at += -(-g.numel() // BLOCK) * BLOCK
+    views = lambda t: [t[o:o + n].view(g.shape) for (o, n), g in zip(spans, grads)]  # noqa: E731
     flat = torch.zeros(at, dtype=torch.float32, device=ring.codec.device)
-    torch._foreach_copy_([flat[o:o + n].view(g.shape) for (o, n), g in zip(spans, grads)], grads)
-    reduced = torch.empty_like(flat)
-    ring.allreduce(flat, reduced, eb_mode, eb, flags=z.OP_AVG | z.CONSISTENT_OWNER)
-    return [reduced[o:o + n].view(g.shape) for (o, n), g in zip(spans, grads)]
+    if at == 0:
+        return views(flat), True
+    torch._foreach_copy_(views(flat), grads)
+    # what is not finite on any rank ends as infinity: a maximum over the ranks could drop a NaN
+    low, high = torch.aminmax(flat)
+    ends = torch.where(torch.isfinite(low) & torch.isfinite(high), torch.stack([-low, high]), float("inf"))
+    if ring.N > 1:
+        ends = ring.link.all_max(ends)
+    low, high = ends.tolist()
+    low = -low
+    if not math.isfinite(low):
+        return views(flat.fill_(float("nan"))), False
+    bound = _bound(low, high, eb_mode, eb, ring.N)
+    if bound is None:
+        return views(flat), True
+    reduced, failed = torch.empty_like(flat), None
+    try:
+        ring.allreduce(flat, reduced, z.EB_ABS, bound, flags=z.OP_AVG | z.CONSISTENT_OWNER)
+    except (z.ZcclError, DegenerateRange) as exc:
+        failed = exc
+    if ring.N > 1:      # a rank's codec tells it alone of what has gone wrong there
+        worst = int(ring.link.all_max(torch.tensor([-getattr(failed, "code", z.E_DEGENERATE) if failed else 0], dtype=torch.int32)).item())
+        if worst and not failed:
+            failed = z.ZcclError(-worst, "exchange, on another rank")
+    if failed:
+        raise failed
+    return views(reduced), True
+
+
+def _bound(low: float, high: float, eb_mode: int, eb: float, ranks: int) -> float | None:
+    """The absolute bound for values from `low` to `high` on all ranks; None where there is nothing to compress.  Refuses what the codec would refuse on the rank that
+    has the largest value, with the codec's arithmetic."""
+    if not (eb > 0) or not math.isfinite(eb):
+        raise ValueError("the error bound must be a positive finite number")
+    f32 = np.float32
+    if eb_mode == z.EB_ABS:
+        bound = f32(eb)
+        with np.errstate(all="ignore"):
+            reciprocal = f32(1) / (bound * f32(0.984375) * f32(2))
+    elif eb_mode == z.EB_REL:
+        if low == high:
+            return None
+        rc, bound, _, reciprocal = z.resolve_range_host(low, high, float(f32(eb)))
+        if rc != z.OK:
+            raise DegenerateRange("relative bound over gradients whose range is too small or not finite")
+    else:
+        raise ValueError("eb_mode")
+    with np.errstate(all="ignore"):
+        if ranks > 1 and not f32(max(-low, high)) * f32(reciprocal) < f32(2.0 ** 30):
+            raise z.ZcclError(z.E_RANGE, "exchange")
+    return float(bound)
 
 
 class AdamW:
@@ -67,14 +131,18 @@ class AdamW:
 
     def step(self, grads=None, max_norm: float | None = None, ring=None, eb_mode: int = z.EB_REL, eb: float = 1e-3, stream=None) -> torch.Tensor | None:
         """One step.  `ring`: exchange the gradients over its ranks first, with this error bound (then on the current stream).  `max_norm`: scale them to
-        that norm at most; returns the norm (float32 [1], on the device).  A step whose norm is not finite changes nothing but `steps`."""
+        that norm at most; returns the norm (float32 [1], on the device).  A step whose norm is not finite changes nothing but `steps`; nor does one whose
+        gradients are not finite on some rank of `ring`, on any of its ranks, with `max_norm` or without."""
         grads = [p.grad for p in self.params] if grads is None else list(grads)
         if any(g is None for g in grads):
             raise ValueError("every parameter needs a gradient")
         if ring is not None:
             if stream is not None:
                 raise ValueError("an exchange runs on the current stream")
-            grads = exchange(ring, grads, eb_mode, eb)
+            grads, finite = _exchange(ring, grads, eb_mode, eb)
+            if not finite:
+                self.steps += 1
+                return None if max_norm is None else torch.full((1,), float("nan"), device=ring.codec.device)
         norm = None if max_norm is None else grad_norm(grads, stream=stream)
         self.steps += 1
         adamw(self.params, grads, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale, self.exp_avg_sq_scale, step=self.steps, lr=self.lr, betas=self.betas, eps=self.eps,

@@ -151,3 +151,74 @@ def test_real_ranks_end_with_the_parameters_of_the_emulated_exchange():
     for r in range(world):
         for a, b in zip(got[r], params + [norm]):
             np.testing.assert_array_equal(a, b.cpu().numpy())
+
+
+def _refusing_worker(rank, world, port, q):
+    os.environ.update(MASTER_ADDR="127.0.0.1", MASTER_PORT=str(port), RANK=str(rank), WORLD_SIZE=str(world))
+    sys.path.insert(0, str(ROOT))
+    try:
+        from paper_2502_18554_b200 import optim, ring, zccl as z
+        torch.cuda.set_device(0)
+        dist.init_process_group("gloo", rank=rank, world_size=world)
+        res = {}
+        for name in ("nan", "inf", "zeros", "out of range", "sum out of range"):
+            params = [p.cuda() for p in _params()]
+            grads = [g.cuda() for g in _gradients(rank)]
+            R = ring.Ring(optim.exchange_elems(params))
+            mode, eb = z.EB_REL, 1e-3
+            if name == "zeros":
+                grads = [torch.zeros_like(g) for g in grads]
+            elif name in ("nan", "inf") and rank == 1:
+                grads[1][3, 4] = float(name)
+            elif name == "out of range":
+                mode, eb = z.EB_ABS, 1e-3
+                if rank == 1:
+                    grads[1][3, 4] = 3e6            # 2^30 steps of this bound are 2.1e6
+            elif name == "sum out of range":
+                mode, eb = z.EB_ABS, 1e-3
+                grads[1][3, 4] = 1.5e6
+            opt = optim.AdamW(params, state_bits=8, seed=5, **HYPER)
+            try:
+                norm = opt.step(grads, max_norm=0.1, ring=R, eb_mode=mode, eb=eb)
+                outcome = "finite" if bool(torch.isfinite(norm)) else "left out"
+            except z.ZcclError as exc:
+                outcome = exc.code
+            res[name] = (outcome, opt.steps, [p.cpu().numpy() for p in params])
+            assert R.codec.ctx.status() == 0
+        q.put((rank, res, None))
+        dist.barrier()
+        dist.destroy_process_group()
+    except Exception as e:
+        import traceback
+        q.put((rank, None, traceback.format_exc()))
+        raise e
+
+
+def test_real_ranks_end_alike_whatever_the_gradients_hold():
+    """Two processes on the one GPU: gradients that are not finite on one rank leave the step out on both, zeros are a step, and what the codec refuses on one rank
+    (as it is, or summed up on the way) is refused by both; parameters stay what they were, and the codec is usable afterwards."""
+    from paper_2502_18554_b200 import build, zccl as z
+    build.build()
+    ctx = mp.get_context("spawn")
+    q = ctx.Queue()
+    port = 28600 + os.getpid() % 500
+    procs = [ctx.Process(target=_refusing_worker, args=(r, 2, port, q)) for r in range(2)]
+    for p in procs:
+        p.start()
+    got = {}
+    for _ in range(2):
+        rank, res, err = q.get(timeout=300)
+        assert err is None, err
+        got[rank] = res
+    for p in procs:
+        p.join(120)
+        assert p.exitcode == 0
+    before = [p.numpy() for p in _params()]
+    for r in range(2):
+        for name, outcome, steps in (("nan", "left out", 1), ("inf", "left out", 1), ("zeros", "finite", 1), ("out of range", z.E_RANGE, 0), ("sum out of range", z.E_RANGE, 0)):
+            assert got[r][name][:2] == (outcome, steps), (name, r, got[r][name][:2])
+            for a, b in zip(got[r][name][2], before):
+                if name == "zeros":     # decayed alone: 1 - lr weight_decay and the product are rounded
+                    np.testing.assert_allclose(a, b.astype(np.float64) * (1 - HYPER["lr"] * HYPER["weight_decay"]), rtol=3 * 2.0 ** -24, atol=0)
+                else:
+                    np.testing.assert_array_equal(a, b)
