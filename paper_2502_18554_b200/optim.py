@@ -144,9 +144,9 @@ class AdamW:
                 self.steps += 1
                 return None if max_norm is None else torch.full((1,), float("nan"), device=ring.codec.device)
         norm = None if max_norm is None else grad_norm(grads, stream=stream)
-        self.steps += 1
-        adamw(self.params, grads, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale, self.exp_avg_sq_scale, step=self.steps, lr=self.lr, betas=self.betas, eps=self.eps,
+        adamw(self.params, grads, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale, self.exp_avg_sq_scale, step=self.steps + 1, lr=self.lr, betas=self.betas, eps=self.eps,
               weight_decay=self.weight_decay, copies=self.copies, norm=norm, max_norm=1.0 if max_norm is None else max_norm, seed=self.seed, stream=stream)
+        self.steps += 1     # not before: a step that is refused has not been
         return norm
 
     def state_dict(self) -> dict:

@@ -222,3 +222,18 @@ def test_real_ranks_end_alike_whatever_the_gradients_hold():
                     np.testing.assert_allclose(a, b.astype(np.float64) * (1 - HYPER["lr"] * HYPER["weight_decay"]), rtol=3 * 2.0 ** -24, atol=0)
                 else:
                     np.testing.assert_array_equal(a, b)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_refused_step_leaves_no_trace(bits):
+    """A step with a gradient of the wrong size is refused; the next one is that of an optimizer that was never given it."""
+    from paper_2502_18554_b200 import optim
+    g = [torch.randn(100, device="cuda"), torch.randn(7, 9, device="cuda")]
+    a, b = (optim.AdamW([torch.ones(100, device="cuda"), torch.ones(7, 9, device="cuda")], state_bits=bits, seed=3) for _ in range(2))
+    for bad in ([g[0]], [g[0], g[1].double()], [g[0][:50], g[1]]):
+        with pytest.raises(ValueError):
+            a.step(bad, max_norm=1.0 if len(bad) == 1 else None)
+    a.step(g, max_norm=1.0)
+    b.step(g, max_norm=1.0)
+    assert a.steps == b.steps == 1 and all(torch.equal(p, q) for p, q in zip(a.params, b.params))
+    assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a.exp_avg + a.exp_avg_sq, b.exp_avg + b.exp_avg_sq))

@@ -246,3 +246,17 @@ def test_the_bound_is_the_codecs():
             optim._bound(0.0, 1.0, z.EB_ABS, eb, 2)
     with pytest.raises(ValueError):
         optim._bound(0.0, 1.0, z.EB_RESOLVED, 1.0, 2)
+
+
+def test_a_refused_step_is_not_counted(monkeypatch):
+    from paper_2502_18554_b200 import optim
+    p = [torch.zeros(5)]
+    o = optim.AdamW(p)
+    with pytest.raises(ValueError):
+        o.step([torch.zeros(5)])                # not on a GPU
+    assert o.steps == 0
+    seen = []
+    monkeypatch.setattr(optim, "adamw", lambda *a, **k: seen.append(k["step"]))
+    o.step([torch.zeros(5)])
+    o.step([torch.zeros(5)])
+    assert seen == [1, 2] and o.steps == 2
