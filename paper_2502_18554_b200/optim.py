@@ -150,10 +150,12 @@ class AdamW:
         return norm
 
     def state_dict(self) -> dict:
-        """Steps so far and the states (the tensors themselves)."""
-        return {"steps": self.steps, "exp_avg": self.exp_avg, "exp_avg_sq": self.exp_avg_sq, "exp_avg_scale": self.exp_avg_scale, "exp_avg_sq_scale": self.exp_avg_sq_scale}
+        """Steps so far, the seed of the roundings and the states (the tensors themselves)."""
+        return {"steps": self.steps, "seed": self.seed, "exp_avg": self.exp_avg, "exp_avg_sq": self.exp_avg_sq, "exp_avg_scale": self.exp_avg_scale, "exp_avg_sq_scale": self.exp_avg_sq_scale}
 
     def load_state_dict(self, state: dict) -> None:
+        """Takes over what state_dict gave, the seed included (where there is none in it, this optimizer's stays): the steps that follow are those that would have followed there."""
+        steps, seed = state["steps"], state.get("seed", self.seed)
         for key in ("exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale"):
             mine, theirs = getattr(self, key), state[key]
             if (mine is None) != (theirs is None) or (mine is not None and [(t.shape, t.dtype) for t in mine] != [(t.shape, t.dtype) for t in theirs]):
@@ -161,4 +163,4 @@ class AdamW:
         for key in ("exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale"):
             for m, t in zip(getattr(self, key) or (), state[key] or ()):
                 m.copy_(t)
-        self.steps = state["steps"]
+        self.steps, self.seed = steps, seed

@@ -237,3 +237,19 @@ def test_a_refused_step_leaves_no_trace(bits):
     b.step(g, max_norm=1.0)
     assert a.steps == b.steps == 1 and all(torch.equal(p, q) for p, q in zip(a.params, b.params))
     assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a.exp_avg + a.exp_avg_sq, b.exp_avg + b.exp_avg_sq))
+
+
+def test_a_run_goes_on_in_an_optimizer_that_was_made_with_another_seed():
+    from paper_2502_18554_b200 import optim
+    gen = torch.Generator().manual_seed(2)
+    grads = [[torch.randn(3000, generator=gen).cuda()] for _ in range(4)]
+    a, b = optim.AdamW([torch.ones(3000, device="cuda")], state_bits=8, seed=3), optim.AdamW([torch.ones(3000, device="cuda")], state_bits=8)
+    for g in grads[:2]:
+        a.step(g)
+    b.load_state_dict(a.state_dict())
+    b.params[0].copy_(a.params[0])
+    for g in grads[2:]:
+        a.step(g)
+        b.step(g)
+        for x, y in zip(a.params + a.exp_avg + a.exp_avg_sq + a.exp_avg_scale, b.params + b.exp_avg + b.exp_avg_sq + b.exp_avg_scale):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))

@@ -260,3 +260,18 @@ def test_a_refused_step_is_not_counted(monkeypatch):
     o.step([torch.zeros(5)])
     o.step([torch.zeros(5)])
     assert seen == [1, 2] and o.steps == 2
+
+
+def test_the_seed_is_saved_and_loaded():
+    from paper_2502_18554_b200 import optim
+    a, b = optim.AdamW([torch.zeros(40)], state_bits=8, seed=11), optim.AdamW([torch.zeros(40)], state_bits=8, seed=4)
+    a.steps = 6
+    state = a.state_dict()
+    b.load_state_dict(state)
+    assert (b.steps, b.seed) == (6, 11)
+    del state["seed"]                           # as saved before seeds were
+    c = optim.AdamW([torch.zeros(40)], state_bits=8, seed=4)
+    c.load_state_dict(state)
+    assert (c.steps, c.seed) == (6, 4)
+    with pytest.raises(KeyError):
+        c.load_state_dict({k: v for k, v in state.items() if k != "steps"})
