@@ -465,7 +465,7 @@ int zccl_mx4_linear(const void* x, int type, size_t m, size_t k, size_t x_pitch,
  *   g' = g * min(1, max_norm / (norm + 1e-6))  where norm is given, else g
  *   m  = beta1 m + (1 - beta1) g'        v = beta2 v + (1 - beta2) g'^2
  *   p  = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
- * in binary32 (sums of products fused, roots and quotients to within 2^-22), p rounded once to its type.  A norm that is negative or not finite leaves parameters, copies and states as they were.
+ * in binary32 (sums of products fused, roots and quotients to within 2^-22), p rounded once to its type; eps is 0 or a normal number of binary32 (2^-126 at least).  A norm that is negative or not finite leaves parameters, copies and states as they were.
  *
  * States in 32 bits are arrays of n floats.  In 8 bits m and r = sqrt(v) are held as E4M3 (n bytes each) with one scale byte e + 127 per
  * block of 32 elements of the tensor (ceil(n / 32) bytes each), e the smallest power of two, from -127 on, at which the block's largest

@@ -3,6 +3,7 @@
 #include "zccl_mx4.cuh"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <new>
 #include <vector>
@@ -354,7 +355,8 @@ __device__ __forceinline__ uint2 pack8(float (&v)[8], const uint32_t (&noise)[8]
     return make_uint2(prmt(prmt(z[0], z[1], 0x0073), prmt(z[2], z[3], 0x0073), 0x5410), prmt(prmt(z[4], z[5], 0x0073), prmt(z[6], z[7], 0x0073), 0x5410));
 }
 
-// Both to within 2^-22.  A root of a subnormal number is one (gradients of 1e-19 square to these); no root is subnormal itself, so no quotient is by one.
+// Both to within 2^-22.  A root of a subnormal number is taken of it as it is (gradients of 1e-19 square to these); no root is subnormal itself and zccl_adamw takes no eps that is, so
+// no quotient is by one: its reciprocal would be infinite, and 0 times that NaN.
 __device__ __forceinline__ float root_of(float v)
 {
     float r;
@@ -698,6 +700,7 @@ int zccl_adamw(const zccl_adamw_tensor* tensors, size_t count, const zccl_adamw_
     if (!type_ok(k.param_type) || !type_ok(k.grad_type) || (k.state_bits != 32 && k.state_bits != 8)) return ZCCL_E_ARG;
     const auto rate_ok = [](double b) { return b >= 0.0 && b < 1.0; };
     if (!rate_ok(k.beta1) || !rate_ok(k.beta2) || !(k.eps >= 0.0) || !std::isfinite(k.eps) || !std::isfinite(k.weight_decay)) return ZCCL_E_ARG;
+    if (k.eps > 0.0 && (float)k.eps < FLT_MIN) return ZCCL_E_ARG;   // see reciprocal_of
     if ((!k.lr_device && !std::isfinite(k.lr)) || (!k.step_device && k.step < 1) || (k.norm && !(k.max_norm > 0.0))) return ZCCL_E_ARG;
     if (((uintptr_t)k.step_device & 7u) || ((uintptr_t)k.lr_device & 3u) || ((uintptr_t)k.norm & 3u)) return ZCCL_E_ARG;
     size_t used = 0, total = 0;

@@ -431,3 +431,24 @@ def test_refusals(optim):
     with pytest.raises(ValueError):
         optim.grad_norm([t(6)[::2]])
     run(optim, {"p": [], "g": [], "m": [], "v": []})                       # nothing to do
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_the_smallest_eps(optim, bits):
+    """Nothing learnt and nothing to learn: 0 / eps is 0 down to the smallest normal number; what is below it is refused."""
+    make = lambda: tensors([64, 5000], torch.float32, torch.float32, bits)  # noqa: E731
+    for eps in (2.0 ** -126, 1e-30, 1e-8):
+        s = make()
+        for key in ("g", "m", "v"):
+            for x in s[key]:
+                x.view(torch.uint8).zero_()
+        before = [p.clone() for p in s["p"]]
+        run(optim, s, eps=eps)
+        for p, q in zip(s["p"], before):
+            assert torch.allclose(p, q * (1 - HYPER["lr"] * HYPER["weight_decay"]), rtol=4 * U, atol=0)
+    for eps in (1e-40, 1e-60):
+        s = make()
+        before = flat_bytes(s)
+        with pytest.raises(RuntimeError):
+            run(optim, s, eps=eps)
+        assert all(torch.equal(a, b) for a, b in zip(before, flat_bytes(s)))

@@ -137,3 +137,14 @@ def test_random_bits_of_the_reference_are_spread():
         u = half.astype(np.float64) / 65536
         assert abs(u.mean() - 0.5) < 5 * np.sqrt(1 / 12 / u.size)
         assert abs(np.corrcoef(u[:-1], u[1:])[0, 1]) < 5 / np.sqrt(u.size)
+
+
+def test_the_step_refuses_an_eps_that_binary32_holds_as_a_subnormal_number(lib):
+    """By such a one nothing can be divided (its reciprocal is no number of binary32); 0 and from 2^-126 on is what the formula is kept for."""
+    from paper_2502_18554_b200 import zccl
+    step = lib.zccl_adamw
+    step.argtypes = [C.POINTER(Tensor), C.c_size_t, C.POINTER(Config), C.c_void_p]
+    nothing = Tensor(None, None, None, None, None, None, None, 0)
+    for eps, want in ((1e-40, zccl.E_ARG), (1e-60, zccl.E_ARG), (2.0 ** -127, zccl.E_ARG), (5e-324, zccl.E_ARG), (2.0 ** -126, zccl.OK), (1e-30, zccl.OK), (0.0, zccl.OK)):
+        k = Config(0, 0, 1, 32, 1e-3, 0.9, 0.999, eps, 0.0, 1, None, None, 0, None, 1.0)
+        assert step(C.byref(nothing), 1, C.byref(k), None) == want, eps
