@@ -317,6 +317,11 @@ bool stream_on(PyObject* o, const at::Tensor& t, void** st)
     if (index != t.device().index()) return refuse("the stream is of another device than the tensors");
     return stream_of(o, st);
 }
+// Tells autograd that a tensor has been written, which may have been saved for a backward pass.
+void written(const at::Tensor& t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 // A list or tuple of tensors, kept alive by its caller.
 struct Tensors {
     PyObject* seq = nullptr;
@@ -435,6 +440,10 @@ PyObject* mx4_quantize(PyObject*, Args a, Py_ssize_t na)
     if (!given) f = new_form(rows, cols, *x.t);
     const int rc = x.quantize(transpose, f.codes.data_ptr(), f.scales.data_ptr(), place.st);
     if (rc != ZCCL_OK) return PyLong_FromLong(rc);
+    if (given) {
+        written(f.codes);
+        written(f.scales);
+    }
     return Py_BuildValue("NNnn", THPVariable_Wrap(f.codes), THPVariable_Wrap(f.scales), (Py_ssize_t)rows, (Py_ssize_t)cols);
 }
 
@@ -486,7 +495,9 @@ PyObject* mx4_dequantize(PyObject*, Args a, Py_ssize_t na)
     Place place;
     if (!place.take(a[6], *codes)) return nullptr;
     const at::Tensor out = given ? *y.t : new_matrix(rows, cols, dt, *codes);
-    return wrapped(zccl_mx4_dequantize(f.codes.data_ptr(), f.scales.data_ptr(), rows, cols, out.data_ptr(), type_of(out), given ? y.pitch : cols, place.st), out);
+    const int rc = zccl_mx4_dequantize(f.codes.data_ptr(), f.scales.data_ptr(), rows, cols, out.data_ptr(), type_of(out), given ? y.pitch : cols, place.st);
+    if (given && rc == ZCCL_OK) written(out);
+    return wrapped(rc, out);
 }
 
 // (a_codes, a_scales, m, b_codes, b_scales, n, k, dtype, y or None, stream) -> y or a status
@@ -507,7 +518,9 @@ PyObject* mx4_matmul(PyObject*, Args a, Py_ssize_t na)
     Place place;
     if (!place.take(a[9], *codes)) return nullptr;
     const at::Tensor out = given ? *y.t : new_matrix(m, n, dt, *codes);
-    return wrapped(zccl_mx4_matmul(l.codes.data_ptr(), l.scales.data_ptr(), m, r.codes.data_ptr(), r.scales.data_ptr(), n, k, out.data_ptr(), type_of(out), given ? y.pitch : n, place.st), out);
+    const int rc = zccl_mx4_matmul(l.codes.data_ptr(), l.scales.data_ptr(), m, r.codes.data_ptr(), r.scales.data_ptr(), n, k, out.data_ptr(), type_of(out), given ? y.pitch : n, place.st);
+    if (given && rc == ZCCL_OK) written(out);
+    return wrapped(rc, out);
 }
 
 // (x, w) or (x, codes, scales, n) -> x W^T in x's type, or a status
@@ -735,13 +748,9 @@ PyObject* adamw(PyObject*, Args a, Py_ssize_t na)
     Place place;
     if (!place.take(a[16], *first)) return nullptr;
     const int rc = zccl_adamw(list.data(), count, &k, place.st);
-    // parameters and copies may have been saved for a backward pass
     for (size_t i = 0; rc == ZCCL_OK && i < count; ++i)
         for (const Tensors* l : {&p, copied ? &copies : nullptr})
-            if (l) {
-                const at::Tensor& x = THPVariable_Unpack(PySequence_Fast_GET_ITEM(l->seq, (Py_ssize_t)i));
-                if (!x.is_inference()) x.unsafeGetTensorImpl()->bump_version();
-            }
+            if (l) written(THPVariable_Unpack(PySequence_Fast_GET_ITEM(l->seq, (Py_ssize_t)i)));
     return PyLong_FromLong(rc);
 }
 
@@ -771,7 +780,9 @@ PyObject* grad_norm(PyObject*, Args a, Py_ssize_t na)
     if (!place.take(a[2], like)) return nullptr;
     const at::Tensor out = given ? *norm : at::Tensor(at::detail::empty_cuda({1}, c10::kFloat, like.device(), c10::nullopt));
     const at::Tensor work = new_bytes(zccl_grad_norm_work(count), like);
-    return wrapped(zccl_grad_norm(at.data(), n.data(), count, type, (float*)out.data_ptr(), work.data_ptr(), place.st), out);
+    const int rc = zccl_grad_norm(at.data(), n.data(), count, type, (float*)out.data_ptr(), work.data_ptr(), place.st);
+    if (given && rc == ZCCL_OK) written(out);
+    return wrapped(rc, out);
 }
 
 // What torch throws (a tensor without memory or strides of its own, no memory left) ends here as a Python exception.

@@ -218,3 +218,38 @@ def test_nothing_to_do(mx):
         assert mx.dequantize(q).shape == (rows, cols)
         q = mx.quantize(torch.zeros(rows, cols, device="cuda"), transpose=True)
         assert mx.dequantize(q).shape == (cols, rows)
+
+
+def test_autograd_is_told_that_an_output_was_written(mx):
+    """A tensor that was saved for a backward pass and then handed in as an output."""
+    x = torch.randn(8, 64, device="cuda")
+    q = mx.quantize(x)
+    weights = torch.ones(8, 64, device="cuda", requires_grad=True)
+
+    def saved(shape):
+        t = torch.randn(shape, device="cuda")
+        return t, (t * weights[:shape[0], :shape[1]]).sum()
+
+    for shape, write in (((8, 64), lambda t: mx.dequantize(q, out=t)), ((8, 8), lambda t: mx.matmul(q, q, out=t))):
+        t, loss = saved(shape)
+        write(t)
+        with pytest.raises(RuntimeError, match="modified by an inplace"):
+            loss.backward()
+    versions = q.codes._version, q.scales._version
+    mx.quantize(x, out=q)
+    assert q.codes._version > versions[0] and q.scales._version > versions[1]
+    with torch.inference_mode():
+        t = torch.empty(8, 64, device="cuda")
+        mx.dequantize(q, out=t)                  # has no version
+    assert torch.equal(t, mx.dequantize(q))
+
+
+def test_autograd_is_told_that_a_norm_was_written(mx):
+    from paper_2502_18554_b200 import optim
+    g = [torch.randn(100, device="cuda")]
+    scale = torch.ones(1, device="cuda", requires_grad=True)
+    norm = optim.grad_norm(g)
+    loss = (norm * scale).sum()
+    optim.grad_norm(g, out=norm)
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        loss.backward()
