@@ -324,3 +324,21 @@ def test_calls_that_read_what_the_call_in_front_writes(mx, dtype):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for p, q in zip(want, got) for a, b in zip(p, q))
     assert mx.status() == 0
+
+
+def test_forward_mode_tangents_are_refused(mx):
+    """There is no forward-mode derivative: a dual tensor raises instead of losing its tangent."""
+    import torch.autograd.forward_ad as fwd
+    x, w = torch.randn(4, 64, device="cuda"), torch.randn(40, 64, device="cuda")
+    q = mx.quantize(w)
+    with fwd.dual_level():
+        dual, dual_w = fwd.make_dual(x, torch.ones_like(x)), fwd.make_dual(w, torch.ones_like(w))
+        for call in (lambda: mx.linear(dual, w), lambda: mx.linear(x, dual_w), lambda: mx.linear(dual, q), lambda: mx.linear(dual[None], q), lambda: mx.quantize(dual),
+                     lambda: mx.quantize_all([x, dual]), lambda: mx.linear_backward(torch.randn(4, 40, device="cuda"), dual, w)):
+            with pytest.raises(ValueError, match="tangent"):
+                call()
+        with pytest.raises((ValueError, RuntimeError, NotImplementedError)):
+            mx.linear(dual, w.clone().requires_grad_())
+        mx.linear(x, w)                                         # others are none the worse for it
+    with torch.no_grad(), pytest.raises(Exception):
+        torch.func.jvp(lambda t: mx.linear(t, w), (x,), (torch.ones_like(x),))
