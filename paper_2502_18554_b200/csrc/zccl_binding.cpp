@@ -10,6 +10,7 @@
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/DynamicTypes.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 
 #include <algorithm>
 #include <vector>
@@ -786,11 +787,12 @@ PyObject* grad_norm(PyObject*, Args a, Py_ssize_t na)
     return wrapped(rc, out);
 }
 
-// What torch throws (a tensor without memory or strides of its own, no memory left) ends here as a Python exception.
+// What torch throws (a tensor without memory or strides of its own, no memory left) ends here as a Python exception.  A trace would take the outputs for constants.
 template <PyObject* (*F)(PyObject*, Args, Py_ssize_t)>
 PyObject* guarded(PyObject* self, Args a, Py_ssize_t na)
 {
     try {
+        if (torch::jit::tracer::isTracing()) return refuse("this call cannot be recorded in a trace"), nullptr;
         return F(self, a, na);
     } catch (const std::exception& e) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());

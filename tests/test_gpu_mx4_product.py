@@ -342,3 +342,14 @@ def test_forward_mode_tangents_are_refused(mx):
         mx.linear(x, w)                                         # others are none the worse for it
     with torch.no_grad(), pytest.raises(Exception):
         torch.func.jvp(lambda t: mx.linear(t, w), (x,), (torch.ones_like(x),))
+
+
+@pytest.mark.filterwarnings("ignore")
+def test_a_trace_is_refused(mx):
+    """A trace would hold the output for the first input as a constant."""
+    x, w = torch.randn(4, 64, device="cuda"), torch.randn(40, 64, device="cuda")
+    q = mx.quantize(w)
+    for call in (lambda t: mx.linear(t, w), lambda t: mx.linear(t, q), lambda t: mx.dequantize(mx.quantize(t)), lambda t: t + mx.matmul(q, q).sum()):
+        with pytest.raises(ValueError, match="trace"):
+            torch.jit.trace(call, (x,))
+    mx.linear(x, q)
