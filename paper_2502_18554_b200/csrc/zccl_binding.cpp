@@ -324,13 +324,28 @@ void written(const at::Tensor& t)
 {
     if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
-// A list or tuple of tensors, kept alive by its caller.
+// A boundary call without the interpreter lock: a launch waits where the GPU's queue is full, and other threads go on meanwhile.
+template <class F>
+int unlocked(F&& f)
+{
+    struct Lock {
+        PyThreadState* const state = PyEval_SaveThread();
+        ~Lock() { PyEval_RestoreThread(state); }
+    } lock;
+    return f();
+}
+// The tensors of a sequence, held for the call: another thread may change a list while the lock is not held.
 struct Tensors {
     PyObject* seq = nullptr;
     ~Tensors() { Py_XDECREF(seq); }
     bool take(PyObject* o)
     {
         seq = PySequence_Fast(o, "expected a sequence of tensors");
+        if (seq && PyList_Check(seq)) {
+            PyObject* const list = seq;
+            seq = PyList_AsTuple(list);
+            Py_DECREF(list);
+        }
         return seq != nullptr;
     }
     size_t count() const { return seq ? (size_t)PySequence_Fast_GET_SIZE(seq) : 0; }
@@ -370,7 +385,11 @@ struct Matrix {
         return true;
     }
     zccl_mx4_job job(bool transpose, void* codes, void* scales) const { return {t->data_ptr(), rows, cols, pitch, transpose, codes, scales}; }
-    int quantize(bool transpose, void* codes, void* scales, void* st) const { return zccl_mx4_quantize(t->data_ptr(), type, rows, cols, pitch, transpose, codes, scales, st); }
+    int quantize(bool transpose, void* codes, void* scales, void* st) const
+    {
+        void* const x = t->data_ptr();
+        return unlocked([&] { return zccl_mx4_quantize(x, type, rows, cols, pitch, transpose, codes, scales, st); });
+    }
 };
 // Forms that a call needs for itself, out of one allocation: each costs the host as much as a small kernel costs the GPU.
 struct Inner {
@@ -398,7 +417,8 @@ struct InnerForms {
 };
 int multiply(const Inner& a, size_t m, const Inner& b, size_t n, size_t k, const at::Tensor& y, void* st)
 {
-    return zccl_mx4_matmul(a.codes, a.scales, m, b.codes, b.scales, n, k, y.data_ptr(), type_of(y), n, st);
+    void* const out = y.data_ptr();
+    return unlocked([&] { return zccl_mx4_matmul(a.codes, a.scales, m, b.codes, b.scales, n, k, out, type_of(y), n, st); });
 }
 // A form that the caller has: bytes of the right number on the right device.
 bool take_form(PyObject* codes, PyObject* scales, size_t rows, size_t cols, const at::Tensor& like, Form* f)
@@ -472,7 +492,7 @@ PyObject* mx4_quantize_all(PyObject*, Args a, Py_ssize_t na)
         f[i] = transpose ? new_form(x[i].cols, x[i].rows, *x[0].t) : new_form(x[i].rows, x[i].cols, *x[0].t);
         jobs[i] = x[i].job(transpose, f[i].codes.data_ptr(), f[i].scales.data_ptr());
     }
-    const int rc = zccl_mx4_quantize_all(jobs.data(), (int)count, x[0].type, place.st);
+    const int rc = unlocked([&] { return zccl_mx4_quantize_all(jobs.data(), (int)count, x[0].type, place.st); });
     if (rc != ZCCL_OK) return PyLong_FromLong(rc);
     PyObject* const out = PyList_New((Py_ssize_t)count);
     for (size_t i = 0; out && i < count; ++i) PyList_SET_ITEM(out, (Py_ssize_t)i, Py_BuildValue("NN", THPVariable_Wrap(f[i].codes), THPVariable_Wrap(f[i].scales)));
@@ -497,7 +517,7 @@ PyObject* mx4_dequantize(PyObject*, Args a, Py_ssize_t na)
     Place place;
     if (!place.take(a[6], *codes)) return nullptr;
     const at::Tensor out = given ? *y.t : new_matrix(rows, cols, dt, *codes);
-    const int rc = zccl_mx4_dequantize(f.codes.data_ptr(), f.scales.data_ptr(), rows, cols, out.data_ptr(), type_of(out), given ? y.pitch : cols, place.st);
+    const int rc = unlocked([&] { return zccl_mx4_dequantize(f.codes.data_ptr(), f.scales.data_ptr(), rows, cols, out.data_ptr(), type_of(out), given ? y.pitch : cols, place.st); });
     if (given && rc == ZCCL_OK) written(out);
     return wrapped(rc, out);
 }
@@ -520,7 +540,9 @@ PyObject* mx4_matmul(PyObject*, Args a, Py_ssize_t na)
     Place place;
     if (!place.take(a[9], *codes)) return nullptr;
     const at::Tensor out = given ? *y.t : new_matrix(m, n, dt, *codes);
-    const int rc = zccl_mx4_matmul(l.codes.data_ptr(), l.scales.data_ptr(), m, r.codes.data_ptr(), r.scales.data_ptr(), n, k, out.data_ptr(), type_of(out), given ? y.pitch : n, place.st);
+    const int rc = unlocked([&] {
+        return zccl_mx4_matmul(l.codes.data_ptr(), l.scales.data_ptr(), m, r.codes.data_ptr(), r.scales.data_ptr(), n, k, out.data_ptr(), type_of(out), given ? y.pitch : n, place.st);
+    });
     if (given && rc == ZCCL_OK) written(out);
     return wrapped(rc, out);
 }
@@ -553,10 +575,12 @@ PyObject* mx4_linear(PyObject*, Args a, Py_ssize_t na)
     if (na == 2) {
         const Inner g = inner[1];
         const zccl_mx4_job both[2] = {w.job(false, g.codes, g.scales), x.job(false, f.codes, f.scales)};
-        rc = zccl_mx4_quantize_all(both, 2, x.type, place.st);
+        rc = unlocked([&] { return zccl_mx4_quantize_all(both, 2, x.type, place.st); });
         if (rc == ZCCL_OK) rc = multiply(f, x.rows, g, n, x.cols, y, place.st);
     } else
-        rc = zccl_mx4_linear(x.t->data_ptr(), x.type, x.rows, x.cols, x.pitch, held.codes.data_ptr(), held.scales.data_ptr(), n, f.codes, f.scales, y.data_ptr(), n, place.st);
+        rc = unlocked([&] {
+            return zccl_mx4_linear(x.t->data_ptr(), x.type, x.rows, x.cols, x.pitch, held.codes.data_ptr(), held.scales.data_ptr(), n, f.codes, f.scales, y.data_ptr(), n, place.st);
+        });
     return wrapped(rc, y);
 }
 
@@ -595,9 +619,9 @@ PyObject* mx4_linear_backward(PyObject*, Args a, Py_ssize_t na)
             jobs[count++] = o.from->job(o.transpose, f.codes, f.scales);
         }
     int rc = ZCCL_OK;
-    if (dy.type == x.type && w.type == x.type) rc = zccl_mx4_quantize_all(jobs, count, x.type, place.st);
+    if (dy.type == x.type && w.type == x.type) rc = unlocked([&] { return zccl_mx4_quantize_all(jobs, count, x.type, place.st); });
     else
-        for (int i = 0; i < count && rc == ZCCL_OK; ++i) rc = zccl_mx4_quantize_all(&jobs[i], 1, types[i], place.st);
+        for (int i = 0; i < count && rc == ZCCL_OK; ++i) rc = unlocked([&] { return zccl_mx4_quantize_all(&jobs[i], 1, types[i], place.st); });
     if (want_x && rc == ZCCL_OK) rc = multiply(inner[0], m, inner[1], k, n, dx, place.st);
     if (want_w && rc == ZCCL_OK) rc = multiply(inner[count - 2], n, inner[count - 1], k, m, dw, place.st);
     if (rc != ZCCL_OK) return PyLong_FromLong(rc);
@@ -749,7 +773,7 @@ PyObject* adamw(PyObject*, Args a, Py_ssize_t na)
     if (PyErr_Occurred()) return nullptr;
     Place place;
     if (!place.take(a[16], *first)) return nullptr;
-    const int rc = zccl_adamw(list.data(), count, &k, place.st);
+    const int rc = unlocked([&] { return zccl_adamw(list.data(), count, &k, place.st); });
     for (size_t i = 0; rc == ZCCL_OK && i < count; ++i)
         for (const Tensors* l : {&p, copied ? &copies : nullptr})
             if (l) written(THPVariable_Unpack(PySequence_Fast_GET_ITEM(l->seq, (Py_ssize_t)i)));
@@ -782,7 +806,7 @@ PyObject* grad_norm(PyObject*, Args a, Py_ssize_t na)
     if (!place.take(a[2], like)) return nullptr;
     const at::Tensor out = given ? *norm : at::Tensor(at::detail::empty_cuda({1}, c10::kFloat, like.device(), c10::nullopt));
     const at::Tensor work = new_bytes(zccl_grad_norm_work(count), like);
-    const int rc = zccl_grad_norm(at.data(), n.data(), count, type, (float*)out.data_ptr(), work.data_ptr(), place.st);
+    const int rc = unlocked([&] { return zccl_grad_norm(at.data(), n.data(), count, type, (float*)out.data_ptr(), work.data_ptr(), place.st); });
     if (given && rc == ZCCL_OK) written(out);
     return wrapped(rc, out);
 }

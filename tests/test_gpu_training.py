@@ -253,3 +253,72 @@ def test_a_run_goes_on_in_an_optimizer_that_was_made_with_another_seed():
         b.step(g)
         for x, y in zip(a.params + a.exp_avg + a.exp_avg_sq + a.exp_avg_scale, b.params + b.exp_avg + b.exp_avg_sq + b.exp_avg_scale):
             assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+def test_other_threads_go_on_while_a_launch_waits():
+    """With the GPU's queue full (it spins for a while) launches wait, and the interpreter lock is not held meanwhile."""
+    import threading
+    import time
+    from paper_2502_18554_b200 import build, mx, optim
+    build.build()
+    x, w = torch.randn(4, 64, device="cuda"), torch.randn(40, 64, device="cuda")
+    q, y = mx.quantize(w), torch.empty(40, 40, device="cuda")
+    state = lambda: [torch.zeros(64, device="cuda")]  # noqa: E731
+    p, m, v, g, norm = state(), state(), state(), state(), torch.zeros(1, device="cuda")
+    calls = [lambda: mx.matmul(q, q, out=y), lambda: mx.quantize(w, out=q), lambda: mx.dequantize(q, out=w), lambda: optim.grad_norm(g, out=norm),
+             lambda: optim.adamw(p, g, m, v, step=1, lr=1e-3), lambda: mx.linear(x, q), lambda: mx.linear(x, w), lambda: mx.linear_backward(torch.zeros(4, 40, device="cuda"), x, w),
+             lambda: mx.quantize_all([x, w])]
+    for call in calls:
+        call()
+    torch.cuda.synchronize()
+    for call in calls:
+        done = threading.Event()
+
+        def work():
+            torch.cuda._sleep(1_500_000_000)         # about 0.8 s
+            for _ in range(2500):                    # more than the queue holds
+                call()
+            done.set()
+
+        thread = threading.Thread(target=work)
+        thread.start()
+        last, gap = time.perf_counter(), 0.0
+        while not done.is_set():
+            time.sleep(0.002)
+            now = time.perf_counter()
+            last, gap = now, max(gap, now - last)
+        thread.join()
+        torch.cuda.synchronize()
+        assert gap < 0.3, gap
+
+
+def test_a_list_that_another_thread_changes():
+    """The tensors of a call are its own, whatever becomes of the lists they came in."""
+    import threading
+    from paper_2502_18554_b200 import build, optim
+    build.build()
+    lists = [[torch.zeros(50, device="cuda") for _ in range(200)] for _ in range(4)]
+    whole = [list(x) for x in lists]
+    stop = threading.Event()
+
+    def change():
+        while not stop.is_set():
+            for x, all_ in zip(lists, whole):
+                del x[100:]
+                x.extend(all_[100:])
+
+    thread = threading.Thread(target=change)
+    thread.start()
+    done = 0
+    try:
+        for _ in range(300):
+            try:
+                optim.adamw(*lists, step=1, lr=1e-3)
+                done += 1
+            except ValueError:                       # lists of different lengths just then
+                pass
+    finally:
+        stop.set()
+        thread.join()
+    torch.cuda.synchronize()
+    assert not any(bool(t.any()) for x in whole for t in x)
