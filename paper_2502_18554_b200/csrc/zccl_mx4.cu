@@ -323,6 +323,8 @@ template <class T>
 int quantize_all(const zccl_mx4_job* jobs, int count, cudaStream_t st)
 {
     MxJobs list;
+    for (int i = 0; i < count; ++i)     // before anything runs
+        if (jobs[i].rows && jobs[i].cols && plan(jobs[i], sizeof(T), list.job[0]) == 0) return ZCCL_E_ARG;
     for (int at = 0; at < count;) {
         unsigned ctas = 0, columns = 0;
         list.count = 0;
@@ -330,7 +332,6 @@ int quantize_all(const zccl_mx4_job* jobs, int count, cudaStream_t st)
             if (jobs[at].rows == 0 || jobs[at].cols == 0) continue;
             MxJob& job = list.job[list.count];
             const unsigned mine = plan(jobs[at], sizeof(T), job);
-            if (mine == 0) return ZCCL_E_ARG;
             if (ctas > kMxMaxGroups - mine) break;
             job.first = ctas;
             ctas += mine;

@@ -148,3 +148,21 @@ def test_the_step_refuses_an_eps_that_binary32_holds_as_a_subnormal_number(lib):
     for eps, want in ((1e-40, zccl.E_ARG), (1e-60, zccl.E_ARG), (2.0 ** -127, zccl.E_ARG), (5e-324, zccl.E_ARG), (2.0 ** -126, zccl.OK), (1e-30, zccl.OK), (0.0, zccl.OK)):
         k = Config(0, 0, 1, 32, 1e-3, 0.9, 0.999, eps, 0.0, 1, None, None, 0, None, 1.0)
         assert step(C.byref(nothing), 1, C.byref(k), None) == want, eps
+
+
+class Job(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("rows", C.c_size_t), ("cols", C.c_size_t), ("pitch", C.c_size_t), ("transpose", C.c_int), ("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the pointers are none")
+@pytest.mark.parametrize("transpose", [0, 1])
+def test_a_matrix_too_large_is_refused_before_anything_runs(lib, transpose):
+    """Behind as many as one launch takes: nothing has been launched, which here, without a GPU, would be another error."""
+    from paper_2502_18554_b200 import zccl
+    call = lib.zccl_mx4_quantize_all
+    call.argtypes = [C.POINTER(Job), C.c_int, C.c_int, C.c_void_p]
+    small, large = Job(4096, 4, 32, 32, 0, 4096, 4096), Job(4096, 1 << 30, 1 << 20, 1 << 20, transpose, 4096, 4096)
+    for before in (0, 1, 8, 9, 16):
+        jobs = (Job * (before + 1))(*[small] * before, large)
+        assert call(jobs, before + 1, 1, None) == zccl.E_ARG, before
+    assert call((Job * 1)(small), 1, 1, None) == zccl.E_CUDA
