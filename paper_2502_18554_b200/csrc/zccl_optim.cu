@@ -5,8 +5,6 @@
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
-#include <new>
-#include <vector>
 
 namespace zccl {
 namespace {
@@ -624,21 +622,20 @@ size_t fill_list(AdamList<CAP>& list, uint32_t& chunks, const zccl_adamw_tensor*
     }
     return i - at;
 }
+// (Lists are up to 32 KB, as arguments of a kernel may be, and stand on the stack: there is no allocation to fail.)
 template <int CAP>
 int run_list(const zccl_adamw_tensor* tensors, size_t count, const zccl_adamw_config& k, const AdamCall& call, cudaStream_t st)
 {
-    AdamList<CAP>* list = new (std::nothrow) AdamList<CAP>;
-    if (!list) return ZCCL_E_ARG;
+    AdamList<CAP> list;
     unsigned long long place = 0;
     int rc = ZCCL_OK;
     for (size_t at = 0; at < count && rc == ZCCL_OK;) {
         uint32_t chunks;
-        at += fill_list(*list, chunks, tensors, count, at, place, (size_t)call.passes * kPass);
+        at += fill_list(list, chunks, tensors, count, at, place, (size_t)call.passes * kPass);
         if (chunks == 0) continue;
-        if (launch_adamw_param(k, *list, chunks, call, st) == cudaSuccess) count_launches(1);
+        if (launch_adamw_param(k, list, chunks, call, st) == cudaSuccess) count_launches(1);
         else rc = ZCCL_E_CUDA;
     }
-    delete list;
     return rc;
 }
 
@@ -648,33 +645,31 @@ constexpr size_t kNormAlone = 4;
 template <int CAP>
 int run_norm(const void* const* g, const size_t* n, size_t count, size_t chunks, int type, float* norm, double* parts, cudaStream_t st)
 {
-    NormList<CAP>* list = new (std::nothrow) NormList<CAP>;
-    if (!list) return ZCCL_E_ARG;
+    NormList<CAP> list;
     uint32_t written = 0;
     cudaError_t e = cudaSuccess;
     bool joined = false;
     for (size_t at = 0; at < count && e == cudaSuccess;) {
-        list->count = 0;
-        list->chunks = 0;
+        list.count = 0;
+        list.chunks = 0;
         const size_t from = at;
-        for (; at < count && list->count < CAP; ++at) {
+        for (; at < count && list.count < CAP; ++at) {
             if (n[at] == 0) continue;
             const size_t mine = (n[at] + kChunk - 1) / kChunk;
-            if (mine > kMostChunks - list->chunks) break;
-            list->g[list->count] = g[at];
-            list->n[list->count] = n[at];
-            list->first[list->count++] = list->chunks;
-            list->chunks += (uint32_t)mine;
+            if (mine > kMostChunks - list.chunks) break;
+            list.g[list.count] = g[at];
+            list.n[list.count] = n[at];
+            list.first[list.count++] = list.chunks;
+            list.chunks += (uint32_t)mine;
         }
-        if (list->chunks == 0) continue;
-        joined = chunks <= kNormAlone && from == 0 && list->chunks == chunks;
-        const uint32_t ctas = joined ? 1u : std::min<uint32_t>(list->chunks, kNormCtas);
+        if (list.chunks == 0) continue;
+        joined = chunks <= kNormAlone && from == 0 && list.chunks == chunks;
+        const uint32_t ctas = joined ? 1u : std::min<uint32_t>(list.chunks, kNormCtas);
         const auto kernel = type == ZCCL_F32 ? norm_parts_kernel<float, CAP> : type == ZCCL_BF16 ? norm_parts_kernel<__nv_bfloat16, CAP> : norm_parts_kernel<__half, CAP>;
-        e = launch_k(kernel, dim3(ctas), dim3(kOptThreads), 0, st, *list, parts + written, joined ? norm : nullptr);
+        e = launch_k(kernel, dim3(ctas), dim3(kOptThreads), 0, st, list, parts + written, joined ? norm : nullptr);
         if (e == cudaSuccess) count_launches(1);
         written += ctas;
     }
-    delete list;
     if (!joined && e == cudaSuccess) {
         e = launch_k(norm_join_kernel, dim3(1), dim3(kOptThreads), 0, st, parts, written, norm);
         if (e == cudaSuccess) count_launches(1);
