@@ -657,13 +657,16 @@ inline bool entry(const Tensors& list, size_t i, c10::ScalarType dt, size_t n, c
 }
 // Whether the tensors of a list share no byte.  Lists are in the order of memory more often than not: only others are sorted.
 struct Apart {
-    uintptr_t end = 0;
+    uintptr_t begin = 0, end = 0;
     bool ordered = true;
     void add(const void* p, size_t bytes)
     {
         ordered &= bytes == 0 || (uintptr_t)p >= end;
+        if (end == 0) begin = (uintptr_t)p;
         if (bytes) end = (uintptr_t)p + bytes;
     }
+    // Lists in the order of memory, one behind the other: none of their tensors can overlap.
+    bool clear_of(const Apart& o) const { return ordered && o.ordered && (end <= o.begin || o.end <= begin); }
     // `at(i)` and `bytes(i)`: where tensor i is and how long
     template <class F, class G>
     bool ok(size_t count, F&& at, G&& bytes) const
@@ -706,7 +709,7 @@ PyObject* adamw(PyObject*, Args a, Py_ssize_t na)
     if (copied && (k.param_type != ZCCL_F32 || k.copy_type == ZCCL_F32)) return refuse("copies are bfloat16 or float16 ones of float32 parameters"), nullptr;
     const c10::ScalarType pt = first->scalar_type(), gt = grad->scalar_type(), state = eight ? c10::ScalarType::Float8_e4m3fn : c10::kFloat;
     std::vector<zccl_adamw_tensor> list(count);
-    Apart apart[6];
+    Apart apart[7];
     const size_t wide = c10::elementSize(pt), state_bytes = c10::elementSize(state);
     for (size_t i = 0; i < count; ++i) {
         zccl_adamw_tensor& s = list[i];
@@ -735,6 +738,7 @@ PyObject* adamw(PyObject*, Args a, Py_ssize_t na)
             apart[5].add(s.copy, 2 * n);
         }
         apart[0].add(s.p, n * wide);
+        apart[6].add(s.g, n * c10::elementSize(gt));
         apart[1].add(s.m, n * state_bytes);
         apart[2].add(s.v, n * state_bytes);
     }
@@ -744,6 +748,19 @@ PyObject* adamw(PyObject*, Args a, Py_ssize_t na)
         !apart[2].ok(count, [&](size_t i) { return list[i].v; }, states) || !apart[3].ok(count, [&](size_t i) { return list[i].m_scale; }, blocks) ||
         !apart[4].ok(count, [&](size_t i) { return list[i].v_scale; }, blocks) || !apart[5].ok(count, [&](size_t i) { return list[i].copy; }, [&](size_t i) { return 2 * list[i].n; }))
         return refuse("two tensors of a list overlap"), nullptr;
+    bool clear = true;
+    for (int i = 1; i < 7; ++i)
+        for (int j = 0; j < i; ++j) clear = clear && apart[i].clear_of(apart[j]);
+    for (const zccl_adamw_tensor& s : list) {
+        if (clear) break;
+        const size_t n = s.n, scales = eight ? (n + ZCCL_BLOCK - 1) / ZCCL_BLOCK : 0;
+        const struct { const void* p; size_t bytes; } arrays[7] = {{s.p, n * wide},          {s.g, n * c10::elementSize(gt)}, {s.m, n * state_bytes}, {s.v, n * state_bytes},
+                                                                   {s.copy, copied ? 2 * n : 0}, {s.m_scale, scales},             {s.v_scale, scales}};
+        for (int i = 1; i < 7; ++i)
+            for (int j = 0; j < i; ++j)
+                if ((uintptr_t)arrays[i].p < (uintptr_t)arrays[j].p + arrays[j].bytes && (uintptr_t)arrays[j].p < (uintptr_t)arrays[i].p + arrays[i].bytes)
+                    return refuse("a parameter, its gradient, states and copy overlap"), nullptr;
+    }
     const auto scalar = [&](PyObject* o, c10::ScalarType dt, const at::Tensor** x) {
         if (!cuda_tensor(o, x)) return false;
         if ((*x)->numel() != 1 || (*x)->scalar_type() != dt || (*x)->device() != first->device()) {

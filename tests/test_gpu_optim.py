@@ -452,3 +452,26 @@ def test_the_smallest_eps(optim, bits):
         with pytest.raises(RuntimeError):
             run(optim, s, eps=eps)
         assert all(torch.equal(a, b) for a, b in zip(before, flat_bytes(s)))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_tensors_that_are_in_two_lists_are_refused(optim, bits):
+    """A parameter's gradient, states, scales and copy share no memory, wherever in the list it stands."""
+    for i in (0, 1, 2):
+        s = tensors([64, 7, 4096], torch.float32, torch.float32, bits)
+        before = flat_bytes(s)
+        other = lambda key, x: {**s, key: [x if j == i else t for j, t in enumerate(s[key])]}  # noqa: E731
+        cases = [other("v", s["m"][i]), {**s, "v": s["m"]}]
+        if bits == 32:
+            cases += [other("g", s["p"][i]), other("m", s["p"][i]), other("v", s["g"][i])]
+        else:
+            cases += [other("vs", s["ms"][i]), other("ms", s["p"][i].view(torch.uint8)[:s["ms"][i].numel()])]
+        for case in cases:
+            with pytest.raises(ValueError, match="overlap"):
+                run(optim, case)
+        copies = [torch.zeros(t.numel(), dtype=torch.bfloat16, device="cuda") for t in s["p"]]
+        copies[i] = s["p"][i].view(torch.bfloat16)[:s["p"][i].numel()]
+        with pytest.raises(ValueError, match="overlap"):
+            run(optim, s, copies=copies)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(before, flat_bytes(s)))
