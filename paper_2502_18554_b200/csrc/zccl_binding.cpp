@@ -286,9 +286,10 @@ bool matrix(PyObject* o, const at::Tensor** t, int* type, size_t* pitch)
     if (*type < 0) return refuse("expected float32, bfloat16 or float16");
     if ((*t)->layout() != c10::kStrided || (*t)->is_neg()) return refuse("expected a dense tensor");
     if ((*t)->_fw_grad(0).defined()) return refuse("a tensor with a forward-mode tangent, which would be lost here");
-    if ((*t)->dim() != 2 || ((*t)->size(1) > 1 && (*t)->stride(1) != 1) || ((*t)->size(0) > 1 && (*t)->stride(0) < (*t)->size(1)))
+    const bool some = (*t)->numel() > 0;     // without elements any strides are good
+    if ((*t)->dim() != 2 || (some && (((*t)->size(1) > 1 && (*t)->stride(1) != 1) || ((*t)->size(0) > 1 && (*t)->stride(0) < (*t)->size(1)))))
         return refuse("expected a matrix with contiguous rows");
-    *pitch = (*t)->size(0) > 1 ? (size_t)(*t)->stride(0) : (size_t)(*t)->size(1);
+    *pitch = some && (*t)->size(0) > 1 ? (size_t)(*t)->stride(0) : (size_t)(*t)->size(1);
     return true;
 }
 // Bytes of exactly this number on the same device.

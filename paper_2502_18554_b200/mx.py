@@ -102,10 +102,10 @@ class _Linear(torch.autograd.Function):
 
 
 def linear(x: torch.Tensor, w: torch.Tensor | Mx4) -> torch.Tensor:
-    """x W^T with both sides in microscaled form, in x's type, on the current stream.  x is [..., k]; `w` is [n, k] of x's type, or already
+    """x W^T with both sides in microscaled form, in x's type, on the current stream.  x is [..., k], rows contiguous; `w` is [n, k] of x's type, or already
     quantised (weights that are laid out once; no gradient then).  With a tensor for `w` this is differentiable, by linear_backward, once and backwards: tensors with
     a forward-mode tangent are refused."""
-    rows = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
+    rows = x if x.dim() == 2 else x.reshape(x.shape[:-1].numel(), x.shape[-1])
     if isinstance(w, Mx4):
         if x.requires_grad and torch.is_grad_enabled():
             raise ValueError("quantised weights are for inference: pass the weights themselves to train, or detach x")

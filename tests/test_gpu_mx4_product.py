@@ -353,3 +353,21 @@ def test_a_trace_is_refused(mx):
         with pytest.raises(ValueError, match="trace"):
             torch.jit.trace(call, (x,))
     mx.linear(x, q)
+
+
+@pytest.mark.parametrize("lead", [(), (3,), (2, 3), (0,), (2, 0, 3)])
+@pytest.mark.parametrize("k", [0, 1, 64])
+def test_layers_of_any_leading_dimensions(mx, lead, k):
+    """Empty ones and rows without elements included: nothing to sum is zeros."""
+    x, w = torch.randn(*lead, k, device="cuda"), torch.randn(5, k, device="cuda")
+    for weights in (w, mx.quantize(w)):
+        y = mx.linear(x, weights)
+        assert y.shape == (*lead, 5)
+        if x.numel() == 0:
+            assert not y.any()
+        else:
+            close(y.reshape(-1, 5), rounded(x.reshape(-1, k)), rounded(w))
+    x.requires_grad_()
+    w.requires_grad_()
+    mx.linear(x, w).sum().backward()
+    assert x.grad.shape == x.shape and w.grad.shape == w.shape
