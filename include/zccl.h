@@ -444,12 +444,15 @@ int zccl_mx4_dequantize(const void* codes, const void* scales, size_t rows, size
  * Product of two operands in this form: y [device, m x n, `pitch` elements from row to row] <- A B^T, A m x k, B n x k, both quantised along
  * k: sums of exact products in binary32 on the tensor cores, each rounded once to `type`.  What is behind the last row and block of the scales
  * has to be 0, as zccl_mx4_quantize leaves it.  The order of the sum depends on the sizes alone: the same call gives the same bits.  k = 0 gives
- * zeros.  Waits inside the kernels are bounded; one that ran out leaves y unspecified and is recorded for zccl_mx4_status, which
- * synchronises `stream`, returns ZCCL_OK or ZCCL_E_TIMEOUT for the current device and clears the record.
+ * zeros.  Waits inside the kernels are bounded (two seconds each); one that ran out leaves y unspecified and is recorded for the device: from then on
+ * zccl_mx4_matmul and zccl_mx4_linear return ZCCL_E_TIMEOUT there and run nothing, until zccl_mx4_status, which synchronises `stream`, returns ZCCL_OK or
+ * ZCCL_E_TIMEOUT for the current device and clears the record.  (Replays of captured calls run all the same: ask zccl_mx4_status behind them.)
  */
 int zccl_mx4_matmul(const void* a_codes, const void* a_scales, size_t m, const void* b_codes, const void* b_scales, size_t n, size_t k,
                     void* y, int type, size_t pitch, void* stream);
 int zccl_mx4_status(void* stream);
+/* Test hook: enqueues one thread that waits, as the products do, for something that never arrives, gives up and records it. */
+int zccl_debug_mx4_wait(void* stream);
 /*
  * A layer with weights in this form, y [m x n] <- Q(x) W^T in x's type (x [m x k, `x_pitch`]): the bits of zccl_mx4_quantize of x along its rows and
  * zccl_mx4_matmul.  x_codes and x_scales are room for the form of an m x k matrix; calls that may run at the same time need one each.  A few rows are

@@ -16,13 +16,11 @@ constexpr int kRows = 128;                    // rows of a tile: the tensor core
 constexpr int kDepth = 256;                   // elements along the contraction per stage: 128 bytes of codes, a row of the swizzle
 constexpr int kRowBytes = kDepth / 2;         // an instruction takes 64 elements, 32 bytes of them
 constexpr int kProductThreads = 192;          // one warp loads, one issues, four read the sums out (eight in pairs of CTAs)
-constexpr uint32_t kWaitLimit = 1u << 22;     // polls of a barrier before giving up
+constexpr uint32_t kWaitLimit = 1u << 19;     // polls of a barrier before giving up: two seconds (a poll that finds nothing takes 4 us; the deepest product that fits
+                                              // the memory is through with a tile in half of one)
 constexpr size_t kMostAcross = 64;            // rows of an output that is stored across
-constexpr uint32_t kStuck = 1u;               // status: a wait ran out
 constexpr int kOutBytes = 64;                 // of a row of the output on its way through shared memory, and their pitch there
 constexpr int kOutPitch = kOutBytes + 16;
-
-__device__ uint32_t g_product_status;
 
 struct Product {
     const unsigned char *r_scales, *c_scales;
@@ -35,30 +33,36 @@ struct Product {
     int early;                                // the rows' operand is complete when the kernel starts (see mx4_split_kernel)
     int wide;                                 // every row of y begins on a 16-byte boundary
     int across;                               // 1: y is stored the other way round, its rows along the kernel's columns
+    uint32_t* stuck;                          // the device's record of a wait that ran out, a word of the host's memory: the next call looks at it without a synchronisation
 };
 
-__device__ __forceinline__ bool wait_for(unsigned long long* bar, uint32_t parity)
+__device__ __noinline__ void record_stuck(uint32_t* stuck)
+{
+    *(volatile uint32_t*)stuck = 1u;
+    __threadfence_system();
+}
+__device__ __forceinline__ bool wait_for(unsigned long long* bar, uint32_t parity, uint32_t* stuck)
 {
     for (uint32_t i = 0; i < kWaitLimit; ++i)
         if (mbar_try_wait(bar, parity)) return true;
-    atomicOr(&g_product_status, kStuck);
+    record_stuck(stuck);
     return false;
 }
-__device__ __forceinline__ bool wait_for_cluster(unsigned long long* bar, uint32_t parity)
+__device__ __forceinline__ bool wait_for_cluster(unsigned long long* bar, uint32_t parity, uint32_t* stuck)
 {
     for (uint32_t i = 0; i < kWaitLimit; ++i)
         if (mbar_try_wait_cluster(bar, parity)) return true;
-    atomicOr(&g_product_status, kStuck);
+    record_stuck(stuck);
     return false;
 }
 // The loading thread's last act: what it has asked for (n stages' worth, `loads`: at this CTA's barriers) lands, and what the tensor core still arrives for at
 // `empty` has arrived, before the memory is given up, whether it is used or not.  `ok`: no wait has run out so far; after one the issuing thread may have given up.
 template <int STAGES>
-__device__ __forceinline__ void settle(unsigned long long* full, unsigned long long* empty, uint32_t n, bool loads, bool ok)
+__device__ __forceinline__ void settle(unsigned long long* full, unsigned long long* empty, uint32_t n, bool loads, bool ok, uint32_t* stuck)
 {
     for (uint32_t i = n < (uint32_t)STAGES ? 0 : n - STAGES; i < n; ++i) {
-        if (loads) ok &= wait_for(&full[i % STAGES], (i / STAGES) & 1);
-        ok = ok && wait_for(&empty[i % STAGES], (i / STAGES) & 1);
+        if (loads) ok &= wait_for(&full[i % STAGES], (i / STAGES) & 1, stuck);
+        ok = ok && wait_for(&empty[i % STAGES], (i / STAGES) & 1, stuck);
     }
 }
 __device__ __forceinline__ unsigned char* on_1024(unsigned char* raw) { return raw + (1024 - (smem_u32(raw) & 1023u)) % 1024; }
@@ -296,20 +300,20 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
             bool ok = true;
             for (uint32_t d = k_begin; d < k_end; ++d, ++n) {
                 const uint32_t s = n % kStages;
-                if (n >= kStages && !(ok = wait_for(&empty[s], (n / kStages - 1) & 1))) break;
+                if (n >= kStages && !(ok = wait_for(&empty[s], (n / kStages - 1) & 1, k.stuck))) break;
                 if (n >= asked) load_rows(s, d);
                 unsigned char* const at = tiles + s * S::kStage;
                 tile_load(at + S::kColAt, &c_map, (int)(d * kRowBytes), (int)c0, &full[s]);
                 bytes_load(at + S::kColScaleAt, k.c_scales + ((size_t)(c0 / kMxBand) * groups + 2 * d) * kMxTileBytes, groups_at(d, k.depth_blocks) * kMxTileBytes, &full[s]);
             }
-            settle<kStages>(full, empty, n, true, ok);
+            settle<kStages>(full, empty, n, true, ok, k.stuck);
         }
     } else if (warp == 1) {
         if (elect_one()) {
             uint32_t n = 0;
             for (uint32_t d = k_begin; d < k_end; ++d, ++n) {
                 const uint32_t s = n % kStages;
-                if (!wait_for(&full[s], (n / kStages) & 1)) break;
+                if (!wait_for(&full[s], (n / kStages) & 1, k.stuck)) break;
                 tcgen05_fence_after();
                 const uint32_t at = smem_u32(tiles) + s * S::kStage;
                 const uint32_t r_scale = tmem + S::kSumColumns + s * S::kScaleColumns, c_scale = r_scale + 8;
@@ -325,9 +329,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
                 tcgen05_commit(&empty[s]);
             }
             tcgen05_commit(&done);
-            wait_for(&done, 0);
+            wait_for(&done, 0, k.stuck);
         }
-    } else if (wait_for(&done, 0)) {
+    } else if (wait_for(&done, 0, k.stuck)) {
         tcgen05_fence_after();
         const uint32_t quarter = warp & 3u, row = quarter * 32 + lane;
         if (BN == 128 && parts == 1) {
@@ -479,16 +483,16 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_token_kernel(const __g
             uint32_t n = asked;
             bool ok = true;
             for (; n < mine; ++n) {
-                if (n >= (uint32_t)kStages && !(ok = wait_for(&empty[n % kStages], (n / kStages - 1) & 1))) break;
+                if (n >= (uint32_t)kStages && !(ok = wait_for(&empty[n % kStages], (n / kStages - 1) & 1, k.stuck))) break;
                 load(n);
             }
-            settle<kStages>(full, empty, n, true, ok);
+            settle<kStages>(full, empty, n, true, ok, k.stuck);
         }
     } else if (warp == 1) {
         if (elect_one()) {
             for (uint32_t n = 0; n < mine; ++n) {
                 const uint32_t s = n % kStages, d = k_begin + n;
-                if (!wait_for(&full[s], (n / kStages) & 1)) break;
+                if (!wait_for(&full[s], (n / kStages) & 1, k.stuck)) break;
                 tcgen05_fence_after();
                 const uint32_t at = smem_u32(tiles) + s * S::kStage, r_scale = tmem + S::S::kSumColumns + s * S::S::kScaleColumns, c_scale = r_scale + 8;
                 for (uint32_t g = 0; g < groups_at(d, k.depth_blocks); ++g) {
@@ -502,9 +506,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_token_kernel(const __g
                 tcgen05_commit(&empty[s]);
             }
             tcgen05_commit(&done);
-            wait_for(&done, 0);
+            wait_for(&done, 0, k.stuck);
         }
-    } else if (wait_for(&done, 0)) {
+    } else if (wait_for(&done, 0, k.stuck)) {
         tcgen05_fence_after();
         const uint32_t quarter = warp & 3u;
         float* const to = reinterpret_cast<float*>(tiles) + quarter * 32 + lane;
@@ -599,7 +603,7 @@ __global__ void __launch_bounds__(PairShape::kThreads, 1) mx4_pair_kernel(const 
                 const int row_band = (int)(rt * 2 + rank), c0 = (int)(ct * BN + rank * (BN / 2));
                 for (uint32_t d = 0; d < depth_tiles; ++d, ++n) {
                     const uint32_t s = n % kStages;
-                    if (n >= kStages && !(ok = wait_for(&empty[s], (n / kStages - 1) & 1))) break;
+                    if (n >= kStages && !(ok = wait_for(&empty[s], (n / kStages - 1) & 1, k.stuck))) break;
                     unsigned char* const at = tiles + s * S::kStage;
                     const uint32_t bar = address_at(&full[s], 0);
                     if (rank == 0) mbar_expect_tx(&full[s], kBoth);
@@ -609,7 +613,7 @@ __global__ void __launch_bounds__(PairShape::kThreads, 1) mx4_pair_kernel(const 
                     scales_load_pair(at + S::kColScaleAt, &c_scale_map, (int)(2 * d), (int)(ct * S::kBands), bar);
                 }
             }
-            settle<kStages>(full, empty, n, rank == 0, ok);   // the first CTA sees both's loads; each sees the arrivals at its own `empty`
+            settle<kStages>(full, empty, n, rank == 0, ok, k.stuck);   // the first CTA sees both's loads; each sees the arrivals at its own `empty`
         }
     } else if (warp == 1) {
         if (rank == 0 && elect_one()) {
@@ -637,11 +641,11 @@ __global__ void __launch_bounds__(PairShape::kThreads, 1) mx4_pair_kernel(const 
             bool ok = true;
             for (uint32_t t = first; t < total && ok; t += stride, ++i) {
                 if (i >= 1) {
-                    if (!(ok = wait_for_cluster(&free_, (i - 1) & 1))) break;
+                    if (!(ok = wait_for_cluster(&free_, (i - 1) & 1, k.stuck))) break;
                     tcgen05_fence_after();
                 }
                 for (uint32_t d = 0; d < depth_tiles; ++d) {
-                    if (!(ok = wait_for(&full[s], parity))) break;
+                    if (!(ok = wait_for(&full[s], parity, k.stuck))) break;
                     tcgen05_fence_after();
                     if (d + 1 < depth_tiles) issue(s, d > 0, 2, 4);
                     else issue(s, d > 0, groups_at(d, k.depth_blocks), steps_at(d, k.depth_blocks));
@@ -654,7 +658,7 @@ __global__ void __launch_bounds__(PairShape::kThreads, 1) mx4_pair_kernel(const 
                 tcgen05_commit_pair(&done);
             }
             tcgen05_commit_own(&drained);
-            wait_for(&drained, 0);
+            wait_for(&drained, 0, k.stuck);
         }
     } else {
         const uint32_t quarter = warp & 3u, half = (warp - 2) >> 2;
@@ -664,7 +668,7 @@ __global__ void __launch_bounds__(PairShape::kThreads, 1) mx4_pair_kernel(const 
             uint32_t rt, ct;
             tile_of(k, t, kBand, rt, ct);
             const uint32_t c = half * (BN / 2);
-            if (!wait_for(&done, i & 1)) break;
+            if (!wait_for(&done, i & 1, k.stuck)) break;
             tcgen05_fence_after();
             store_columns_any<BN / 2>(k, out, tmem + c + (quarter * 32 << 16), (rt * 2 + rank) * kRows + quarter * 32, ct * BN + c, [&] {
                 __syncwarp();
@@ -681,6 +685,15 @@ __global__ void __launch_bounds__(PairShape::kThreads, 1) mx4_pair_kernel(const 
     if (warp == 1) tmem_free_pair(tmem, S::kColumns);
 }
 
+// A test's: waits, as the products do, for a barrier that nothing arrives at.
+__global__ void mx4_waiting_kernel(uint32_t* stuck)
+{
+    __shared__ unsigned long long bar;
+    pdl_enter();
+    mbar_init(&bar, 1);
+    wait_for(&bar, 0, stuck);
+}
+
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
                               CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 constexpr int kMaxDevices = 64;
@@ -689,7 +702,9 @@ EncodeFn g_product_encode = nullptr;
 struct ProductDevice {
     bool ready = false;
     int sms = 0, pairs = 0;       // pairs of CTAs that are resident together
+    uint32_t* stuck = nullptr;    // see Product
 };
+bool is_stuck(const ProductDevice& d) { return *(volatile const uint32_t*)d.stuck != 0; }
 ProductDevice g_product_dev[kMaxDevices];
 
 template <int BN>
@@ -737,6 +752,17 @@ cudaError_t product_device(const ProductDevice** out)
         e = cudaOccupancyMaxActiveClusters(&d.pairs, mx4_pair_kernel, &cfg);
         if (e != cudaSuccess) return e;
         if (d.pairs < 1) return cudaErrorNotSupported;
+        if (!d.stuck) {
+            // also where the first call is one that is captured
+            cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+            if ((e = cudaThreadExchangeStreamCaptureMode(&mode)) != cudaSuccess) return e;
+            void* word = nullptr;
+            e = cudaHostAlloc(&word, sizeof(uint32_t), cudaHostAllocPortable | cudaHostAllocMapped);
+            cudaThreadExchangeStreamCaptureMode(&mode);
+            if (e != cudaSuccess) return e;
+            d.stuck = (uint32_t*)word;
+            *d.stuck = 0;
+        }
         d.ready = true;
     }
     *out = &d;
@@ -826,6 +852,7 @@ bool tokens(const T* x, int type, size_t m, size_t k, size_t x_pitch, const void
     p.type = type;
     p.wide = (uintptr_t)y % 16 == 0 && pitch * sizeof(T) % 16 == 0;
     p.across = 1;
+    p.stuck = dev->stuck;
     p.depth_blocks = (uint32_t)mx_blocks(k);
     p.rows = (uint32_t)n;
     p.cols = (uint32_t)m;
@@ -849,7 +876,9 @@ int multiply(const void* a_codes, const void* a_scales, size_t m, const void* b_
     if (!aligned16(a_codes) || !aligned16(a_scales) || !aligned16(b_codes) || !aligned16(b_scales)) return ZCCL_E_ARG;
     const ProductDevice* dev;
     if (product_device(&dev) != cudaSuccess) return ZCCL_E_CUDA;
+    if (is_stuck(*dev)) return ZCCL_E_TIMEOUT;
     Product p{};
+    p.stuck = dev->stuck;
     p.y = y;
     p.pitch = pitch;
     p.type = type;
@@ -898,6 +927,9 @@ int zccl_mx4_linear(const void* x, int type, size_t m, size_t k, size_t x_pitch,
     if (type < ZCCL_F32 || type > ZCCL_F16 || !aligned16(w_codes) || !aligned16(w_scales) || !aligned16(x_codes) || !aligned16(x_scales) || pitch < n || x_pitch < k) return ZCCL_E_ARG;
     const size_t element = type == ZCCL_F32 ? 4 : 2;
     if (!x || !y || (uintptr_t)x % element || (uintptr_t)y % element) return ZCCL_E_ARG;
+    const ProductDevice* dev;
+    if (product_device(&dev) != cudaSuccess) return ZCCL_E_CUDA;
+    if (is_stuck(*dev)) return ZCCL_E_TIMEOUT;
     cudaStream_t st = (cudaStream_t)stream;
     int rc = ZCCL_OK;
     if (type == ZCCL_F32 ? tokens((const float*)x, type, m, k, x_pitch, w_codes, w_scales, n, y, pitch, st, rc)
@@ -909,14 +941,18 @@ int zccl_mx4_linear(const void* x, int type, size_t m, size_t k, size_t x_pitch,
 
 int zccl_mx4_status(void* stream)
 {
-    cudaStream_t st = (cudaStream_t)stream;
-    uint32_t bits = 0;
-    const uint32_t zero = 0;
-    if (cudaMemcpyFromSymbolAsync(&bits, g_product_status, sizeof bits, 0, cudaMemcpyDeviceToHost, st) != cudaSuccess) return ZCCL_E_CUDA;
-    if (cudaStreamSynchronize(st) != cudaSuccess) return ZCCL_E_CUDA;
-    if (!bits) return ZCCL_OK;
-    if (cudaMemcpyToSymbolAsync(g_product_status, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) return ZCCL_E_CUDA;
+    const ProductDevice* dev;
+    if (product_device(&dev) != cudaSuccess || cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess) return ZCCL_E_CUDA;
+    if (!is_stuck(*dev)) return ZCCL_OK;
+    *(volatile uint32_t*)dev->stuck = 0;
     return ZCCL_E_TIMEOUT;
+}
+
+int zccl_debug_mx4_wait(void* stream)
+{
+    const ProductDevice* dev;
+    if (product_device(&dev) != cudaSuccess) return ZCCL_E_CUDA;
+    return launched(launch_k(mx4_waiting_kernel, dim3(1), dim3(1), 0, (cudaStream_t)stream, dev->stuck));
 }
 
 }  // extern "C"

@@ -84,8 +84,14 @@ def matmul(a: Mx4, b: Mx4, dtype: torch.dtype = torch.bfloat16, out: torch.Tenso
 
 
 def status(stream=None) -> int:
-    """zccl_mx4_status of the current device: waits for `stream`; z.OK or z.E_TIMEOUT."""
+    """zccl_mx4_status of the current device: waits for `stream`; z.OK, or z.E_TIMEOUT where a wait inside a product has run out since it was last asked.  Until
+    it is asked, products and layers on that device raise ZcclError with that code."""
     return int(z.lib().zccl_mx4_status(z._stream_ptr(stream)))
+
+
+def debug_wait(stream=None) -> None:
+    """Test hook: a wait that runs out (zccl_debug_mx4_wait)."""
+    z._check(z.lib().zccl_debug_mx4_wait(z._stream_ptr(stream)), "zccl_debug_mx4_wait")
 
 
 class _Linear(torch.autograd.Function):

@@ -34,7 +34,7 @@ EXPORTS = [
     "zccl_compress_host", "zccl_decompress_host", "zccl_compress_noalloc", "zccl_debug_skip_publish",
     "zccl_debug_set_launch_counter", "zccl_debug_first_tile", "zccl_debug_tile_counters",
     "zccl_debug_ring_streams", "zccl_debug_store_pause", "zccl_debug_leave_before",
-    "zccl_mx4_code_bytes", "zccl_mx4_scale_bytes", "zccl_mx4_quantize", "zccl_mx4_quantize_all", "zccl_mx4_dequantize", "zccl_mx4_matmul", "zccl_mx4_linear", "zccl_mx4_status",
+    "zccl_mx4_code_bytes", "zccl_mx4_scale_bytes", "zccl_mx4_quantize", "zccl_mx4_quantize_all", "zccl_mx4_dequantize", "zccl_mx4_matmul", "zccl_mx4_linear", "zccl_mx4_status", "zccl_debug_mx4_wait",
     "zccl_adamw", "zccl_grad_norm_work", "zccl_grad_norm",
 ]
 
@@ -103,6 +103,7 @@ def lib():
             getattr(L, name).argtypes = [sz, sz]
             getattr(L, name).restype = sz
         L.zccl_mx4_status.argtypes = [vp]
+        L.zccl_debug_mx4_wait.argtypes = [vp]
         L.zccl_grad_norm_work.argtypes = [sz]
         L.zccl_grad_norm_work.restype = sz
         _lib = L

@@ -371,3 +371,46 @@ def test_layers_of_any_leading_dimensions(mx, lead, k):
     w.requires_grad_()
     mx.linear(x, w).sum().backward()
     assert x.grad.shape == x.shape and w.grad.shape == w.shape
+
+
+def test_a_wait_that_ran_out_is_told_by_the_next_call(mx):
+    """Recorded by a thread that waits for nothing: products and layers are refused until the record has been read, and go on afterwards; other calls run."""
+    from paper_2502_18554_b200 import zccl as z
+    x, w = torch.randn(4, 64, device="cuda"), torch.randn(40, 64, device="cuda")
+    q = mx.quantize(w)
+    want = mx.matmul(q, q), mx.linear(x, q), mx.linear(x, w)
+    assert mx.status() == z.OK
+    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    start.record()
+    mx.debug_wait()
+    end.record()
+    torch.cuda.synchronize()
+    assert start.elapsed_time(end) < 10_000
+    for call in (lambda: mx.matmul(q, q), lambda: mx.linear(x, q), lambda: mx.linear(x, w), lambda: mx.linear_backward(torch.zeros(4, 40, device="cuda"), x, w)):
+        with pytest.raises(z.ZcclError) as e:
+            call()
+        assert e.value.code == z.E_TIMEOUT
+    assert torch.equal(mx.quantize(w).codes, q.codes)
+    assert mx.status() == z.E_TIMEOUT and mx.status() == z.OK
+    assert all(torch.equal(a, b) for a, b in zip(want, (mx.matmul(q, q), mx.linear(x, q), mx.linear(x, w))))
+
+
+def test_the_first_product_of_a_process_may_be_a_captured_one():
+    """What a device is prepared with is prepared then, too."""
+    import subprocess
+    import sys
+    from pathlib import Path
+    program = """
+import torch
+from paper_2502_18554_b200 import mx
+x, w = torch.randn(300, 128, device="cuda"), torch.randn(400, 128, device="cuda")
+graph = torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph):
+    y = mx.linear(x, w)
+graph.replay()
+assert torch.equal(y, mx.linear(x, w)) and mx.status() == 0
+print("captured")
+"""
+    r = subprocess.run([sys.executable, "-c", program], cwd=Path(__file__).resolve().parent.parent, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
