@@ -322,9 +322,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) mx4_split_kernel(const __g
                     tcgen05_copy_scales(c_scale + 4 * g, scales_descriptor(at + S::kColScaleAt + g * kMxTileBytes));
                 }
                 const unsigned long long r_codes = operand_descriptor(at), c_codes = operand_descriptor(at + S::kColAt);
-                const uint32_t steps = steps_at(d, k.depth_blocks), shift = BN < kMxBand ? (c0 % kMxBand) / 32 : 0;
+                const uint32_t steps = steps_at(d, k.depth_blocks);
                 for (uint32_t j = 0; j < steps; ++j)
-                    tcgen05_mma_mx4(tmem, r_codes + 2 * j, c_codes + 2 * j, mx4_instruction(kRows, BN, (j & 1) * 2), r_scale + 4 * (j / 2), c_scale + 4 * (j / 2) + shift,
+                    tcgen05_mma_mx4(tmem, r_codes + 2 * j, c_codes + 2 * j, mx4_instruction(kRows, BN, (j & 1) * 2), r_scale + 4 * (j / 2), c_scale + 4 * (j / 2),
                                     n > 0 || j > 0);
                 tcgen05_commit(&empty[s]);
             }
@@ -804,11 +804,12 @@ int launched(cudaError_t e)
     if (e == cudaSuccess) count_launches(1);
     return e == cudaSuccess ? ZCCL_OK : ZCCL_E_CUDA;
 }
+// Tiles narrower than a tile of scales (128) are for outputs that one of them is wide enough for: their scales begin where the tile of scales does.
 template <int BN>
 int launch_split(const Sides& s, Product k, unsigned parts, cudaStream_t st)
 {
     CUtensorMap r, c;
-    if (!set_tiles(k, s, kRows, BN)) return ZCCL_E_ARG;
+    if (!set_tiles(k, s, kRows, BN) || (BN < kMxBand && k.col_tiles > 1)) return ZCCL_E_ARG;
     if (!operand_map(&r, s.r_codes, s.rows, k.depth_blocks, kRows) || !operand_map(&c, s.c_codes, s.cols, k.depth_blocks, BN)) return ZCCL_E_CUDA;
     return launched(launch_cluster(parts, mx4_split_kernel<BN>, dim3(k.row_tiles * k.col_tiles * parts), dim3(kProductThreads), SplitShape<BN>::kBytes, st, r, c, k));
 }
