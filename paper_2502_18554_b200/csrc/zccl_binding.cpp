@@ -7,6 +7,7 @@
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <c10/util/SmallVector.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/DynamicTypes.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -337,20 +338,26 @@ int unlocked(F&& f)
 }
 // The tensors of a sequence, held for the call: another thread may change a list while the lock is not held.
 struct Tensors {
-    PyObject* seq = nullptr;
-    ~Tensors() { Py_XDECREF(seq); }
+    c10::SmallVector<PyObject*, 48> held;
+    Tensors() = default;
+    Tensors(const Tensors&) = delete;
+    Tensors& operator=(const Tensors&) = delete;
+    ~Tensors()
+    {
+        for (PyObject* o : held) Py_DECREF(o);
+    }
     bool take(PyObject* o)
     {
-        seq = PySequence_Fast(o, "expected a sequence of tensors");
-        if (seq && PyList_Check(seq)) {
-            PyObject* const list = seq;
-            seq = PyList_AsTuple(list);
-            Py_DECREF(list);
-        }
-        return seq != nullptr;
+        PyObject* const seq = PySequence_Fast(o, "expected a sequence of tensors");
+        if (!seq) return false;
+        PyObject** const items = PySequence_Fast_ITEMS(seq);
+        held.assign(items, items + PySequence_Fast_GET_SIZE(seq));
+        for (PyObject* t : held) Py_INCREF(t);
+        Py_DECREF(seq);
+        return true;
     }
-    size_t count() const { return seq ? (size_t)PySequence_Fast_GET_SIZE(seq) : 0; }
-    bool at(size_t i, const at::Tensor** t) const { return cuda_tensor(PySequence_Fast_GET_ITEM(seq, (Py_ssize_t)i), t); }
+    size_t count() const { return held.size(); }
+    bool at(size_t i, const at::Tensor** t) const { return cuda_tensor(held[i], t); }
 };
 // ---- microscaled 4-bit floating point.  Outputs are allocated here, on the stream that the call runs on: through Python the small
 // allocations of a call took longer than its kernels.
@@ -482,14 +489,14 @@ PyObject* mx4_quantize_all(PyObject*, Args a, Py_ssize_t na)
     std::vector<Form> f(count);
     std::vector<zccl_mx4_job> jobs(count);
     for (size_t i = 0; i < count; ++i) {
-        if (!x[i].take(PySequence_Fast_GET_ITEM(xs.seq, (Py_ssize_t)i))) return nullptr;
+        if (!x[i].take(xs.held[i])) return nullptr;
         if (x[i].type != x[0].type || x[i].t->device() != x[0].t->device()) return refuse("all matrices of a call are of one type and on one device"), nullptr;
     }
     if (count == 0) return PyList_New(0);
     Place place;
     if (!place.take(a[2], *x[0].t)) return nullptr;
     for (size_t i = 0; i < count; ++i) {
-        const bool transpose = PyObject_IsTrue(PySequence_Fast_GET_ITEM(ts.seq, (Py_ssize_t)i)) == 1;
+        const bool transpose = PyObject_IsTrue(ts.held[i]) == 1;
         f[i] = transpose ? new_form(x[i].cols, x[i].rows, *x[0].t) : new_form(x[i].rows, x[i].cols, *x[0].t);
         jobs[i] = x[i].job(transpose, f[i].codes.data_ptr(), f[i].scales.data_ptr());
     }
@@ -646,7 +653,7 @@ bool refuse_entry(const Tensors& list, size_t i, c10::ScalarType dt, size_t n, c
 }
 inline bool entry(const Tensors& list, size_t i, c10::ScalarType dt, size_t n, const at::Tensor& like, const at::Tensor** t)
 {
-    PyObject* const o = PySequence_Fast_GET_ITEM(list.seq, (Py_ssize_t)i);
+    PyObject* const o = list.held[i];
     if (THPVariable_Check(o)) {
         const at::Tensor& x = THPVariable_Unpack(o);
         if (x.scalar_type() == dt && (size_t)x.numel() == n && x.is_contiguous() && x.device() == like.device()) {
@@ -711,7 +718,7 @@ PyObject* adamw(PyObject*, Args a, Py_ssize_t na)
     const c10::ScalarType pt = first->scalar_type(), gt = grad->scalar_type(), state = eight ? c10::ScalarType::Float8_e4m3fn : c10::kFloat;
     std::vector<zccl_adamw_tensor> list(count);
     Apart apart[7];
-    const size_t wide = c10::elementSize(pt), state_bytes = c10::elementSize(state);
+    const size_t wide = c10::elementSize(pt), grad_bytes = c10::elementSize(gt), state_bytes = c10::elementSize(state);
     for (size_t i = 0; i < count; ++i) {
         zccl_adamw_tensor& s = list[i];
         if (!p.at(i, &t)) return nullptr;
@@ -739,7 +746,7 @@ PyObject* adamw(PyObject*, Args a, Py_ssize_t na)
             apart[5].add(s.copy, 2 * n);
         }
         apart[0].add(s.p, n * wide);
-        apart[6].add(s.g, n * c10::elementSize(gt));
+        apart[6].add(s.g, n * grad_bytes);
         apart[1].add(s.m, n * state_bytes);
         apart[2].add(s.v, n * state_bytes);
     }
@@ -755,7 +762,7 @@ PyObject* adamw(PyObject*, Args a, Py_ssize_t na)
     for (const zccl_adamw_tensor& s : list) {
         if (clear) break;
         const size_t n = s.n, scales = eight ? (n + ZCCL_BLOCK - 1) / ZCCL_BLOCK : 0;
-        const struct { const void* p; size_t bytes; } arrays[7] = {{s.p, n * wide},          {s.g, n * c10::elementSize(gt)}, {s.m, n * state_bytes}, {s.v, n * state_bytes},
+        const struct { const void* p; size_t bytes; } arrays[7] = {{s.p, n * wide},          {s.g, n * grad_bytes}, {s.m, n * state_bytes}, {s.v, n * state_bytes},
                                                                    {s.copy, copied ? 2 * n : 0}, {s.m_scale, scales},             {s.v_scale, scales}};
         for (int i = 1; i < 7; ++i)
             for (int j = 0; j < i; ++j)
@@ -794,7 +801,7 @@ PyObject* adamw(PyObject*, Args a, Py_ssize_t na)
     const int rc = unlocked([&] { return zccl_adamw(list.data(), count, &k, place.st); });
     for (size_t i = 0; rc == ZCCL_OK && i < count; ++i)
         for (const Tensors* l : {&p, copied ? &copies : nullptr})
-            if (l) written(THPVariable_Unpack(PySequence_Fast_GET_ITEM(l->seq, (Py_ssize_t)i)));
+            if (l) written(THPVariable_Unpack(l->held[i]));
     return PyLong_FromLong(rc);
 }
 
