@@ -264,6 +264,13 @@ bool refuse(const char* what)
     PyErr_SetString(PyExc_ValueError, what);
     return false;
 }
+// Whether an object is true; false with a Python error set where it has no answer.
+bool truth(PyObject* o, bool* is)
+{
+    const int t = PyObject_IsTrue(o);
+    *is = t == 1;
+    return t >= 0;
+}
 int type_of(const at::Tensor& t)
 {
     switch (t.scalar_type()) {
@@ -460,7 +467,8 @@ PyObject* mx4_quantize(PyObject*, Args a, Py_ssize_t na)
     if (!nargs_are(na, 5)) return nullptr;
     Matrix x;
     if (!x.take(a[0])) return nullptr;
-    const bool transpose = PyObject_IsTrue(a[1]) == 1;
+    bool transpose;
+    if (!truth(a[1], &transpose)) return nullptr;
     const size_t rows = transpose ? x.cols : x.rows, cols = transpose ? x.rows : x.cols;
     Form f;
     const bool given = a[2] != Py_None;
@@ -496,7 +504,8 @@ PyObject* mx4_quantize_all(PyObject*, Args a, Py_ssize_t na)
     Place place;
     if (!place.take(a[2], *x[0].t)) return nullptr;
     for (size_t i = 0; i < count; ++i) {
-        const bool transpose = PyObject_IsTrue(ts.held[i]) == 1;
+        bool transpose;
+        if (!truth(ts.held[i], &transpose)) return nullptr;
         f[i] = transpose ? new_form(x[i].cols, x[i].rows, *x[0].t) : new_form(x[i].rows, x[i].cols, *x[0].t);
         jobs[i] = x[i].job(transpose, f[i].codes.data_ptr(), f[i].scales.data_ptr());
     }
@@ -601,7 +610,8 @@ PyObject* mx4_linear_backward(PyObject*, Args a, Py_ssize_t na)
     const size_t m = x.rows, k = x.cols, n = w.rows;
     if (dy.rows != m || dy.cols != n || w.cols != k) return refuse("sizes of the gradient, the input and the weights do not belong together"), nullptr;
     if (dy.t->device() != x.t->device() || w.t->device() != x.t->device()) return refuse("all tensors of a call are on one device"), nullptr;
-    const bool want_x = PyObject_IsTrue(a[3]) == 1, want_w = PyObject_IsTrue(a[4]) == 1;
+    bool want_x, want_w;
+    if (!truth(a[3], &want_x) || !truth(a[4], &want_w)) return nullptr;
     Place place;
     if (!place.take(Py_None, *x.t)) return nullptr;
     at::Tensor dx, dw;

@@ -253,3 +253,12 @@ def test_autograd_is_told_that_a_norm_was_written(mx):
     optim.grad_norm(g, out=norm)
     with pytest.raises(RuntimeError, match="modified by an inplace"):
         loss.backward()
+
+
+def test_an_option_that_is_neither_true_nor_false(mx):
+    """What its truth value raises is what the call raises."""
+    x = torch.randn(4, 64, device="cuda")
+    many = np.array([1, 2])
+    for call in (lambda: mx.quantize(x, transpose=many), lambda: mx.quantize_all([x], [many]), lambda: mx.linear_backward(x, x, torch.randn(64, 64, device="cuda"), (many, True))):
+        with pytest.raises(ValueError):
+            call()

@@ -414,3 +414,21 @@ print("captured")
 """
     r = subprocess.run([sys.executable, "-c", program], cwd=Path(__file__).resolve().parent.parent, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("m", [1, 20, 300])
+def test_weights_that_were_written_just_before(mx, m):
+    """Weights quantised anew into the same memory, and a layer right behind: the product asks for them before x is through."""
+    gen = torch.Generator().manual_seed(m)
+    ws = [torch.randn(900, 2000, generator=gen).cuda() for _ in range(4)]
+    x = torch.randn(m, 2000, generator=gen).cuda()
+    want = [mx.linear(x, mx.quantize(w)) for w in ws]
+    q = mx.empty(900, 2000, "cuda")
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        for w in ws:
+            mx.quantize(w, out=q)
+            got.append(mx.linear(x, q))
+    torch.cuda.synchronize()
+    assert all(torch.equal(want[i % 4], y) for i, y in enumerate(got)) and mx.status() == 0
