@@ -735,10 +735,12 @@ int zccl_adamw(const zccl_adamw_tensor* tensors, size_t count, const zccl_adamw_
     call.max_norm = (float)k.max_norm;
     call.copy_type = k.copy_type;
     // Small models are spread over the SMs; large ones have chunks of several passes, whose first loads alone are not covered by work.  Of two, four and eight
-    // passes 64 Mi parameters with states in 32 bits took 326, 317 and 328 us (more is left at the end), 128 Mi with 8 bits 285, 266 and 257.
+    // passes 64 Mi parameters with states in 32 bits took 326, 317 and 328 us (more is left at the end).  With states in 8 bits and 16-bit parameters four and eight
+    // took (290 tensors) 77.8 and 77.8 us for 32 Mi, 143.4 and 139.3 for 64 Mi, 270 and 260 for 128 Mi, 1078 and 1032 for 512 Mi, one tensor 1 to 2 % less with eight; with
+    // binary32 parameters eight took 1 to 3 % longer from 16 to 512 Mi (128 Mi: 336 and 340 us).
     call.passes = 1;
     while (call.passes < 4 && total / kPass > (size_t)kChunksWanted * call.passes) call.passes *= 2;
-    if (k.state_bits == 8 && total / kPass >= (size_t)32 * kChunksWanted) call.passes = 8;
+    if (k.state_bits == 8 && k.param_type != ZCCL_F32 && total / kPass >= (size_t)32 * kChunksWanted) call.passes = 8;
     if (used <= (size_t)kFewTensors) return run_list<kFewTensors>(tensors, count, k, call, (cudaStream_t)stream);
     if (used <= (size_t)kMoreTensors) return run_list<kMoreTensors>(tensors, count, k, call, (cudaStream_t)stream);
     return run_list<kManyTensors>(tensors, count, k, call, (cudaStream_t)stream);

@@ -475,3 +475,17 @@ def test_tensors_that_are_in_two_lists_are_refused(optim, bits):
             run(optim, s, copies=copies)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(before, flat_bytes(s)))
+
+
+@pytest.mark.parametrize("param", [torch.float32, torch.float16])
+def test_a_step_of_many_elements_is_that_of_few_in_every_type(optim, param):
+    """As test_a_step_of_many_elements_is_that_of_few: elements are divided among CTAs in another way from 64 Mi of 16 bits on, and not of binary32."""
+    n, more = 5_000_011, (1 << 26) - 5_000_011
+    make = lambda: tensors([n], param, torch.bfloat16, 8, seed=5)  # noqa: E731
+    s, twin = make(), make()
+    run(optim, s, seed=2)
+    other = {key: torch.zeros(more, dtype=x[0].dtype, device="cuda") for key, x in twin.items() if key in ("p", "g", "m", "v")}
+    other |= {key: torch.zeros(-(-more // 32), dtype=torch.uint8, device="cuda") for key in ("ms", "vs")}
+    run(optim, {key: x + [other[key]] for key, x in twin.items() if key in other}, seed=2)
+    for key in other:
+        assert torch.equal(s[key][0].view(torch.uint8), twin[key][0].view(torch.uint8)), key
