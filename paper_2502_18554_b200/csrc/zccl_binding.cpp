@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <c10/util/SmallVector.h>
@@ -840,8 +841,8 @@ PyObject* grad_norm(PyObject*, Args a, Py_ssize_t na)
     Place place;
     if (!place.take(a[2], like)) return nullptr;
     const at::Tensor out = given ? *norm : at::Tensor(at::detail::empty_cuda({1}, c10::kFloat, like.device(), c10::nullopt));
-    const at::Tensor work = new_bytes(zccl_grad_norm_work(count), like);
-    const int rc = unlocked([&] { return zccl_grad_norm(at.data(), n.data(), count, type, (float*)out.data_ptr(), work.data_ptr(), place.st); });
+    const c10::DataPtr work = c10::cuda::CUDACachingAllocator::get()->allocate(zccl_grad_norm_work(count));   // of the stream that place made current
+    const int rc = unlocked([&] { return zccl_grad_norm(at.data(), n.data(), count, type, (float*)out.data_ptr(), work.get(), place.st); });
     if (given && rc == ZCCL_OK) written(out);
     return wrapped(rc, out);
 }
