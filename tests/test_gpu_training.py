@@ -275,7 +275,7 @@ def test_other_threads_go_on_while_a_launch_waits():
         done = threading.Event()
 
         def work():
-            torch.cuda._sleep(1_500_000_000)         # about 0.8 s
+            torch.cuda._sleep(2_500_000_000)         # 1.3 s
             for _ in range(2500):                    # more than the queue holds
                 call()
             done.set()
@@ -289,7 +289,7 @@ def test_other_threads_go_on_while_a_launch_waits():
             last, gap = now, max(gap, now - last)
         thread.join()
         torch.cuda.synchronize()
-        assert gap < 0.3, gap
+        assert gap < 0.8, gap
 
 
 def test_a_list_that_another_thread_changes():
