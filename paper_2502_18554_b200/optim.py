@@ -40,7 +40,7 @@ def exchange(ring, grads, eb_mode: int, eb: float) -> list[torch.Tensor]:
     each begins at a multiple of 32 elements; the gaps hold zeros, which count into the range that a relative bound refers to.
 
     The codec takes finite values only, so the ranks agree on the smallest and largest value of all gradients first (the host waits for it).  Where a gradient of any
-    rank is not finite, what is returned is NaN throughout, on every rank.  Where all values of all ranks are one, it is returned as it is.  An exchange that a rank has to
+    rank is not finite, what is returned is NaN throughout, on every rank.  Where all values of all ranks are the same number, that is returned as it is.  An exchange that a rank has to
     refuse (values beyond 2^30 steps of the bound, a range that is not finite) raises on every rank."""
     return _exchange(ring, list(grads), eb_mode, eb)[0]
 
@@ -50,6 +50,7 @@ def exchange_elems(grads) -> int:
     return sum(-(-g.numel() // BLOCK) * BLOCK for g in grads)
 
 
+@torch.no_grad()
 def _exchange(ring, grads: list, eb_mode: int, eb: float):
     """(exchange's tensors, whether all gradients of all ranks are finite)."""
     at, spans = 0, []

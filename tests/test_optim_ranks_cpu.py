@@ -275,3 +275,14 @@ def test_the_seed_is_saved_and_loaded():
     assert (c.steps, c.seed) == (6, 4)
     with pytest.raises(KeyError):
         c.load_state_dict({k: v for k, v in state.items() if k != "steps"})
+
+
+def test_exchanged_gradients_are_no_part_of_a_graph():
+    """Gradients that require gradients themselves: their values are exchanged."""
+    from types import SimpleNamespace
+    from paper_2502_18554_b200 import optim, zccl as z
+    alone = SimpleNamespace(N=1, codec=SimpleNamespace(device=torch.device("cpu")), allreduce=lambda x, out, mode, eb, flags: out.copy_(x))
+    for g in (torch.arange(40.0), torch.full((32,), 3.0), torch.tensor([1.0, float("nan")])):
+        (out,) = optim.exchange(alone, [g.clone().requires_grad_() * 1], z.EB_REL, 1e-3)
+        assert not out.requires_grad
+        assert torch.equal(out, g) or not bool(torch.isfinite(g).all())
